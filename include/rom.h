@@ -445,6 +445,94 @@ ROM_API int rom_hybrid_stack_forward(const rom_dims *dims, int32_t d_ff, const r
                              void *hip_stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * A few tokens: the projections of the recurrent step and a whole FFN-MoE layer in the form that one
+ * token of each of up to ROM_FEW_TOKENS sequences wants.  Such a call is one pass over the weights of
+ * the picked experts, so its time is their bytes: they may be held in 4 bits.
+ *
+ * Weights in 4 bits.  A stack of matrices T [n_mats, rows, cols], its columns in groups of `group` (32,
+ * 64 or 128; a last group may be shorter), becomes a code of 4 bits per weight and a bf16 scale per row
+ * and group:
+ *   s     = bf16(max |w| over the group / 6), to nearest even
+ *   code  = sign << 3 | m, m the E2M1 number (0, 0.5, 1, 1.5, 2, 3, 4, 6) nearest to |w| / s, ties to
+ *           the even m, 6 above it; decided by comparing |w| with s times the midpoints, which is exact
+ *   value = +-E2M1(m) * s       (exact in fp32)
+ * s == 0: every value is 0.  A group with a NaN or an infinity: s = NaN, all of its values are NaN.
+ * Layout (one buffer of rom_q4_bytes() bytes; rows padded to a multiple of 16, columns to one of 128,
+ * with zeros): first the codes, [n_mats][rows/16][cols/128][q 4][r 16][j 4][4 bytes] = the eight codes of row
+ * r, columns 32 j + 8 q + (0 .. 7), low nibble first (what a lane of the matrix instruction multiplies: 16 bytes
+ * of each lane, 1 KiB together); then the scales, bf16 [n_mats][rows/16][cols/group][16].
+ * rows and cols are positive multiples of 8 up to 2^20, n_mats is 1 to 64.  */
+#define ROM_FEW_TOKENS 256
+
+/* Bytes of the packed stack (0 if the sizes are not supported).  host-only */
+ROM_API size_t rom_q4_bytes(int32_t n_mats, int32_t rows, int32_t cols, int32_t group);
+
+/*   w T [n_mats, rows, cols], w_q4 rom_q4_bytes() bytes, both 16-byte aligned (device); dtype ROM_DTYPE_* of w.
+ * rom_q4_unpack writes the values the codes stand for (rounded once for bf16): the weights of a prefill
+ * that is to agree with the steps behind it. */
+ROM_API int rom_q4_pack(int dtype, const void *w, int32_t n_mats, int32_t rows, int32_t cols, int32_t group, void *w_q4,
+                        void *hip_stream);
+ROM_API int rom_q4_unpack(int dtype, const void *w_q4, int32_t n_mats, int32_t rows, int32_t cols, int32_t group, void *w,
+                          void *hip_stream);
+
+/* Routed projection with 4-bit weights, the indicator sums of Eq. (10)-(12) over a few tokens:
+ *   out[n, :] = residual[n, :] + row_scale[n] * sum_k gate[n, k] * (W[expert_idx[n, k]] x[n, :])
+ *   w_q4        packed stack [n_mats, rows, cols];  x T [N, cols];  out T [N, rows], must not alias x
+ *   expert_idx  i32 [N, top_k] as rom_route writes it, or NULL (n_mats and top_k 1: one matrix for all).  The
+ *               same expert may appear twice in a row; an index outside [0, n_mats) contributes nothing.
+ *   gate        f32 [N, top_k] or NULL (1);  row_scale f32 [N] or NULL (1);  residual T [N, rows] or NULL (0),
+ *               may be out
+ *   ws          rom_q4_project_workspace_bytes(), 256-byte aligned (may be NULL where that is 0)
+ * Sums in fp32, one rounding to T.  top_k is 1 to 8, N at most ROM_FEW_TOKENS (ROM_E_UNSUPPORTED beyond);
+ * N == 0 is a successful no-op.  Repeated calls give identical bits; a token's result does not depend on
+ * the other tokens of a call of the same N. */
+ROM_API size_t rom_q4_project_workspace_bytes(int32_t rows, int32_t top_k, int64_t N);
+ROM_API int rom_q4_project(int dtype, const void *w_q4, int32_t n_mats, int32_t rows, int32_t cols, int32_t group,
+                           const void *x, int64_t N, int32_t top_k, const int32_t *expert_idx, const float *gate,
+                           const float *row_scale, const void *residual, void *out, void *ws, size_t ws_bytes,
+                           void *hip_stream);
+
+/* The FFN-MoE layer of rom_ffn_moe_forward for a few tokens: pre-norm, gate | up, SwiGLU, down, gate-weighted sum
+ * and skip in two launches (three with top_k > 1 and more than 8 slots), straight from the routing
+ * decision, without its grouping.
+ *   w            q4_group 0: as rom_ffn_moe_forward takes them (w_gate_up in the packed row order).  q4_group
+ *                32, 64 or 128: both packed by rom_q4_pack with that group (w_gate_up after
+ *                rom_ffn_pack_gate_up: [E, 2*d_ff, d_model] and [E, d_model, d_ff])
+ *   expert_idx   i32 [N, K], gate f32 [N, K]: as rom_route, a layer call or a step left them; expert_idx as above
+ *   pre_norm, eps, add_skip, x, out   as rom_ffn_moe_forward
+ *   ws           rom_ffn_step_workspace_bytes(dims, d_ff, N), 256-byte aligned
+ * SiLU(gate) * up is rounded to T between the launches; every sum is fp32.  N at most ROM_FEW_TOKENS. */
+ROM_API size_t rom_ffn_step_workspace_bytes(const rom_dims *dims, int32_t d_ff, int64_t N);
+ROM_API int rom_ffn_moe_step(const rom_dims *dims, int32_t d_ff, const rom_ffn_weights *w, int32_t q4_group, int pre_norm,
+                             float eps, int add_skip, const void *x, int64_t N, const int32_t *expert_idx,
+                             const float *gate, void *out, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* rom_step and rom_block_step with the two projections that make up most of a layer's weights in 4 bits:
+ * w->w_in and w->w_out are packed by rom_q4_pack with q4_group (w_in [E, 2*d_inner, d_model], folded with
+ * the norm's scale first for the block; w_out [E, d_model, d_inner]), everything else is as it was.
+ *   ws   rom_step_q4_workspace_bytes(dims, B): a step's workspace (rom_ws_layout holds) and what the
+ *        projections need behind it;  B at most ROM_FEW_TOKENS */
+ROM_API size_t rom_step_q4_workspace_bytes(const rom_dims *dims, int64_t B);
+ROM_API int rom_step_q4(const rom_dims *dims, const rom_weights *w, int32_t q4_group, const void *x, int64_t B,
+                        float *conv_state, float *ssm_state, void *out, void *ws, size_t ws_bytes, void *hip_stream);
+ROM_API int rom_block_step_q4(const rom_dims *dims, const rom_weights *w, int32_t q4_group, const float *norm_weight,
+                              float eps, const void *x, int64_t B, float *conv_state, float *ssm_state, void *out,
+                              void *ws, size_t ws_bytes, void *hip_stream);
+
+/* One new token per sequence through the hybrid stack of rom_hybrid_stack_forward: x, out, tmp T [B, d_model], the
+ * [n_layers, B, ...] states updated in place.  q4_group 0: the weights of rom_hybrid_stack_forward; 32, 64 or
+ * 128: w_in, w_out and both FFN weights of every layer are packed by rom_q4_pack with that group (B at most
+ * ROM_FEW_TOKENS then).  Every FFN-MoE block runs on the decision of the RoM block in front of it.
+ *   ws      rom_workspace_bytes(dims, B, 1), with q4_group rom_step_q4_workspace_bytes(dims, B)
+ *   ffn_ws  rom_hybrid_step_ffn_workspace_bytes(dims, d_ff, B, q4_group), distinct from ws (may be NULL if no layer has
+ *           an FFN) */
+ROM_API size_t rom_hybrid_step_ffn_workspace_bytes(const rom_dims *dims, int32_t d_ff, int64_t B, int32_t q4_group);
+ROM_API int rom_hybrid_stack_step(const rom_dims *dims, int32_t d_ff, const rom_block *blocks, const rom_ffn_weights *ffns,
+                                  int32_t q4_group, int ffn_pre_norm, int n_layers, float eps, const void *x, int64_t B,
+                                  float *conv_state, float *ssm_state, void *out, void *tmp, void *ws, size_t ws_bytes,
+                                  void *ffn_ws, size_t ffn_ws_bytes, void *hip_stream);
+
+/* ---------------------------------------------------------------------------------------------
  * RoM on a Mamba2 layer (Sec. 5.2, Table 3; the paragraph on streamlined SSMs: every major projection
  * of the block becomes a mixture of experts under the one shared router).  The paper prints no
  * equations for this variant; what is computed (readings: the published Mamba2 layer, routed the

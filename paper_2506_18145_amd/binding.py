@@ -132,6 +132,35 @@ def load_library() -> ctypes.CDLL:
     lib.rom_block_forward_train.restype = ctypes.c_int
     lib.rom_block_forward_train.argtypes = [ctypes.POINTER(RomDims), ctypes.POINTER(_RomWeights), P, F32, P, I64, I64, P, P,
                                             SZ, P]
+    I32 = ctypes.c_int32
+    lib.rom_q4_bytes.restype = SZ
+    lib.rom_q4_bytes.argtypes = [I32, I32, I32, I32]
+    lib.rom_q4_pack.restype = ctypes.c_int
+    lib.rom_q4_pack.argtypes = [ctypes.c_int, P, I32, I32, I32, I32, P, P]
+    lib.rom_q4_unpack.restype = ctypes.c_int
+    lib.rom_q4_unpack.argtypes = [ctypes.c_int, P, I32, I32, I32, I32, P, P]
+    lib.rom_q4_project_workspace_bytes.restype = SZ
+    lib.rom_q4_project_workspace_bytes.argtypes = [I32, I32, I64]
+    lib.rom_q4_project.restype = ctypes.c_int
+    lib.rom_q4_project.argtypes = [ctypes.c_int, P, I32, I32, I32, I32, P, I64, I32, P, P, P, P, P, P, SZ, P]
+    lib.rom_ffn_step_workspace_bytes.restype = SZ
+    lib.rom_ffn_step_workspace_bytes.argtypes = [ctypes.POINTER(RomDims), I32, I64]
+    lib.rom_ffn_moe_step.restype = ctypes.c_int
+    lib.rom_ffn_moe_step.argtypes = [ctypes.POINTER(RomDims), I32, ctypes.POINTER(_RomFfnWeights), I32, ctypes.c_int, F32,
+                                     ctypes.c_int, P, I64, P, P, P, P, SZ, P]
+    lib.rom_step_q4_workspace_bytes.restype = SZ
+    lib.rom_step_q4_workspace_bytes.argtypes = [ctypes.POINTER(RomDims), I64]
+    lib.rom_step_q4.restype = ctypes.c_int
+    lib.rom_step_q4.argtypes = [ctypes.POINTER(RomDims), ctypes.POINTER(_RomWeights), I32, P, I64, P, P, P, P, SZ, P]
+    lib.rom_block_step_q4.restype = ctypes.c_int
+    lib.rom_block_step_q4.argtypes = [ctypes.POINTER(RomDims), ctypes.POINTER(_RomWeights), I32, P, F32, P, I64, P, P, P, P,
+                                      SZ, P]
+    lib.rom_hybrid_step_ffn_workspace_bytes.restype = SZ
+    lib.rom_hybrid_step_ffn_workspace_bytes.argtypes = [ctypes.POINTER(RomDims), I32, I64, I32]
+    lib.rom_hybrid_stack_step.restype = ctypes.c_int
+    lib.rom_hybrid_stack_step.argtypes = [ctypes.POINTER(RomDims), I32, ctypes.POINTER(_RomBlock),
+                                          ctypes.POINTER(_RomFfnWeights), I32, ctypes.c_int, ctypes.c_int, F32, P, I64, P, P,
+                                          P, P, P, SZ, P, SZ, P]
     lib.rom_fold_norm.restype = ctypes.c_int
     lib.rom_fold_norm.argtypes = [ctypes.POINTER(RomDims), P, P, P, P]
     lib.rom_block_forward.restype = ctypes.c_int
@@ -542,6 +571,164 @@ def rom_probe(kind: int, p0: int, p1: int, n_blocks: int, iters: int, scratch: t
            "rom_probe")
 
 
+# ---- a few tokens: weights in 4 bits, routed projection, FFN-MoE step, steps with 4-bit weights
+
+ROM_FEW_TOKENS = 256
+
+
+def _expect(t: Optional[torch.Tensor], what: str, dtype, shape, device) -> None:
+    """Type, shape, layout and device of a tensor that a kernel is about to read or write through its pointer."""
+    if t is None:
+        return
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
+        raise RomError(f"{what}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype} "
+                       f"{tuple(t.shape)} on {t.device}")
+
+
+def _on_current_device(device) -> None:
+    """The calls go to the current device's current stream."""
+    if device.type != "cuda" or (device.index is not None and device.index != torch.cuda.current_device()):
+        raise RomError(f"tensors on {device}, which is not the current device")
+
+
+def _keep_if_captured(kept: list, *buffers) -> None:
+    """A buffer that a captured call uses has to outlive the holder's next, larger one: the graph goes on using it."""
+    if torch.cuda.is_current_stream_capturing():
+        kept.extend(b for b in buffers if b is not None and not any(b is k for k in kept))
+
+
+def _dtype_code(dtype) -> int:
+    if dtype == torch.bfloat16:
+        return ROM_DTYPE_BF16
+    if dtype == torch.float32:
+        return ROM_DTYPE_F32
+    raise RomError(f"{dtype}: bfloat16 or float32 is wanted")
+
+
+def rom_q4_bytes(n_mats: int, rows: int, cols: int, group: int) -> int:
+    return int(load_library().rom_q4_bytes(n_mats, rows, cols, group))
+
+
+def rom_q4_pack(w: torch.Tensor, group: int, w_q4: torch.Tensor) -> None:
+    """w [n_mats, rows, cols] -> w_q4 uint8 [rom_q4_bytes(...)]"""
+    n, rows, cols = w.shape
+    _on_current_device(w.device)
+    _expect(w_q4, "w_q4", torch.uint8, (rom_q4_bytes(n, rows, cols, group),), w.device)
+    _check(load_library().rom_q4_pack(_dtype_code(w.dtype), _ptr(w), n, rows, cols, group, _ptr(w_q4), _stream()), "rom_q4_pack")
+
+
+def rom_q4_unpack(w_q4: torch.Tensor, group: int, w: torch.Tensor) -> None:
+    """w_q4 -> w [n_mats, rows, cols], the values that the codes stand for"""
+    n, rows, cols = w.shape
+    _on_current_device(w.device)
+    _expect(w_q4, "w_q4", torch.uint8, (rom_q4_bytes(n, rows, cols, group),), w.device)
+    _check(load_library().rom_q4_unpack(_dtype_code(w.dtype), _ptr(w_q4), n, rows, cols, group, _ptr(w), _stream()),
+           "rom_q4_unpack")
+
+
+def rom_q4_project_workspace_bytes(rows: int, top_k: int, n_tokens: int) -> int:
+    return int(load_library().rom_q4_project_workspace_bytes(rows, top_k, n_tokens))
+
+
+def rom_q4_project(dtype, w_q4, n_mats, rows, cols, group, x, n_tokens, top_k, expert_idx, gate, row_scale, residual, out, ws):
+    code = load_library().rom_q4_project(
+        dtype, _ptr(w_q4), n_mats, rows, cols, group, _ptr(x), n_tokens, top_k, _ptr(expert_idx), _ptr(gate),
+        _ptr(row_scale), _ptr(residual), _ptr(out), _ptr(ws), _nbytes(ws), _stream())
+    _check(code, "rom_q4_project")
+
+
+def rom_ffn_step_workspace_bytes(dims, d_ff: int, n_tokens: int) -> int:
+    return int(load_library().rom_ffn_step_workspace_bytes(ctypes.byref(dims), d_ff, n_tokens))
+
+
+def rom_ffn_moe_step(dims, d_ff, w_gate_up, w_down, q4_group, pre_norm, eps, add_skip, x, n_tokens, expert_idx, gate, out, ws):
+    w = _RomFfnWeights(_ptr(w_gate_up), _ptr(w_down))
+    code = load_library().rom_ffn_moe_step(
+        ctypes.byref(dims), d_ff, ctypes.byref(w), q4_group, int(bool(pre_norm)), eps, int(bool(add_skip)), _ptr(x),
+        n_tokens, _ptr(expert_idx), _ptr(gate), _ptr(out), _ptr(ws), _nbytes(ws), _stream())
+    _check(code, "rom_ffn_moe_step")
+
+
+def rom_step_q4_workspace_bytes(dims, B: int) -> int:
+    return int(load_library().rom_step_q4_workspace_bytes(ctypes.byref(dims), B))
+
+
+def rom_step_q4(dims, weights, q4_group, x, B, conv_state, ssm_state, out, ws):
+    code = load_library().rom_step_q4(
+        ctypes.byref(dims), ctypes.byref(_weights_struct(weights)), q4_group, _ptr(x), B, _ptr(conv_state), _ptr(ssm_state),
+        _ptr(out), _ptr(ws), _nbytes(ws), _stream())
+    _check(code, "rom_step_q4")
+
+
+def rom_block_step_q4(dims, weights, q4_group, norm_weight, eps, x, B, conv_state, ssm_state, out, ws):
+    code = load_library().rom_block_step_q4(
+        ctypes.byref(dims), ctypes.byref(_weights_struct(weights)), q4_group, _ptr(norm_weight), eps, _ptr(x), B,
+        _ptr(conv_state), _ptr(ssm_state), _ptr(out), _ptr(ws), _nbytes(ws), _stream())
+    _check(code, "rom_block_step_q4")
+
+
+def rom_hybrid_step_ffn_workspace_bytes(dims, d_ff: int, B: int, q4_group: int) -> int:
+    return int(load_library().rom_hybrid_step_ffn_workspace_bytes(ctypes.byref(dims), d_ff, B, q4_group))
+
+
+def rom_hybrid_stack_step(dims, d_ff, blocks, ffns, q4_group, ffn_pre_norm, eps, x, B, conv_state, ssm_state, out, tmp, ws,
+                          ffn_ws):
+    code = load_library().rom_hybrid_stack_step(
+        ctypes.byref(dims), d_ff, blocks, ffns, q4_group, int(bool(ffn_pre_norm)), len(blocks), eps, _ptr(x), B,
+        _ptr(conv_state), _ptr(ssm_state), _ptr(out), _ptr(tmp), _ptr(ws), _nbytes(ws), _ptr(ffn_ws), _nbytes(ffn_ws),
+        _stream())
+    _check(code, "rom_hybrid_stack_step")
+
+
+class RomQ4Weight:
+    """A stack of matrices [n_mats, rows, cols] held in 4 bits with a scale per row and `group` columns.  The calls of one
+    holder share its workspace: they go to one stream, or wait for each other."""
+
+    def __init__(self, packed: torch.Tensor, n_mats: int, rows: int, cols: int, group: int = 64):
+        need = rom_q4_bytes(n_mats, rows, cols, group)
+        if need == 0:
+            raise RomError(f"rom_q4_bytes returned 0: unsupported sizes [{n_mats}, {rows}, {cols}] in groups of {group}")
+        _expect(packed, "packed", torch.uint8, (need,), packed.device)
+        self.packed, self.n_mats, self.rows, self.cols, self.group = packed, n_mats, rows, cols, group
+        self.device = packed.device
+        self._ws: Dict[int, torch.Tensor] = {}      # by top_k, for ROM_FEW_TOKENS tokens: never replaced
+
+    @classmethod
+    def pack(cls, w: torch.Tensor, group: int = 64) -> "RomQ4Weight":
+        """w: bf16 or fp32, [n_mats, rows, cols] or one matrix [rows, cols]."""
+        w = w.unsqueeze(0) if w.dim() == 2 else w
+        packed = torch.empty(rom_q4_bytes(*w.shape, group), dtype=torch.uint8, device=w.device)
+        out = cls(packed, *w.shape, group)
+        rom_q4_pack(w, group, packed)
+        return out
+
+    def unpack(self, dtype=torch.bfloat16) -> torch.Tensor:
+        w = torch.empty((self.n_mats, self.rows, self.cols), dtype=dtype, device=self.device)
+        rom_q4_unpack(self.packed, self.group, w)
+        return w
+
+    def project(self, x: torch.Tensor, expert_idx: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                row_scale: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """residual + row_scale * sum_k gate[:, k] * (W[expert_idx[:, k]] x) for x [N, cols] (rom_q4_project)."""
+        n, k = x.shape[0], expert_idx.shape[1] if expert_idx is not None else 1
+        if out is None:
+            out = torch.empty((n, self.rows), dtype=x.dtype, device=x.device)
+        _on_current_device(self.device)
+        _expect(x, "x", x.dtype, (n, self.cols), self.device)
+        _expect(expert_idx, "expert_idx", torch.int32, (n, k), self.device)
+        _expect(gate, "gate", torch.float32, (n, k), self.device)
+        _expect(row_scale, "row_scale", torch.float32, (n,), self.device)
+        _expect(residual, "residual", x.dtype, (n, self.rows), self.device)
+        _expect(out, "out", x.dtype, (n, self.rows), self.device)
+        if k not in self._ws:
+            self._ws[k] = torch.empty(rom_q4_project_workspace_bytes(self.rows, k, ROM_FEW_TOKENS), dtype=torch.uint8,
+                                      device=self.device)
+        rom_q4_project(_dtype_code(x.dtype), self.packed, self.n_mats, self.rows, self.cols, self.group, x, n, k, expert_idx,
+                       gate, row_scale, residual, out, self._ws[k])
+        return out
+
+
 class RomLayer:
     """Holds one layer's parameters on the GPU plus a workspace, and forwards to the C ABI."""
 
@@ -570,6 +757,52 @@ class RomLayer:
         self._bwd_ws: Optional[torch.Tensor] = None
         self._blk_bwd_ws: Optional[torch.Tensor] = None
         self._block_weights: Optional[Dict[str, Optional[torch.Tensor]]] = None
+        self._q4: Dict[tuple, Dict[str, Optional[torch.Tensor]]] = {}
+        self._kept: list = []
+
+    def q4_weights(self, group: int = 64, block: bool = False) -> Dict[str, Optional[torch.Tensor]]:
+        """The parameters step_q4 (block: block_step_q4, the pre-norm's scale folded in first) takes: w_in and w_out
+        in 4 bits, packed once, everything else shared with the plain layer."""
+        if (group, block) not in self._q4:
+            w = dict(self.block_weights() if block else self.weights)
+            w["w_in"] = RomQ4Weight.pack(w["w_in"], group).packed
+            w["w_out"] = RomQ4Weight.pack(w["w_out"], group).packed
+            self._q4[(group, block)] = w
+        return self._q4[(group, block)]
+
+    def workspace_q4(self, B: int) -> torch.Tensor:
+        need = rom_step_q4_workspace_bytes(self.dims, B)
+        if need == 0:
+            raise RomError(f"rom_step_q4_workspace_bytes returned 0: unsupported dims or more than {ROM_FEW_TOKENS} sequences")
+        if self._ws is None or self._ws.numel() < need:
+            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        _keep_if_captured(self._kept, self._ws)
+        return self._ws
+
+    def _check_step(self, x, conv_state, ssm_state, out):
+        B, d = x.shape[0], self.dims
+        _on_current_device(x.device)
+        _expect(x, "x", self.tdtype, (B, d.d_model), x.device)
+        _expect(out, "out", self.tdtype, (B, d.d_model), x.device)
+        _expect(conv_state, "conv_state", torch.float32, (B, d.d_inner, d.d_conv - 1), x.device)
+        _expect(ssm_state, "ssm_state", torch.float32, (B, d.d_inner, d.d_state), x.device)
+
+    def step_q4(self, x: torch.Tensor, conv_state: torch.Tensor, ssm_state: torch.Tensor, group: int = 64,
+                out: Optional[torch.Tensor] = None):
+        """step with w_in and w_out in 4 bits (rom_step_q4): up to ROM_FEW_TOKENS sequences."""
+        out = torch.empty_like(x) if out is None else out
+        self._check_step(x, conv_state, ssm_state, out)
+        rom_step_q4(self.dims, self.q4_weights(group), group, x, x.shape[0], conv_state, ssm_state, out,
+                    self.workspace_q4(max(x.shape[0], 1)))
+        return out
+
+    def block_step_q4(self, x: torch.Tensor, conv_state: torch.Tensor, ssm_state: torch.Tensor, group: int = 64,
+                      out: Optional[torch.Tensor] = None, eps: float = 1e-5):
+        out = torch.empty_like(x) if out is None else out
+        self._check_step(x, conv_state, ssm_state, out)
+        rom_block_step_q4(self.dims, self.q4_weights(group, block=True), group, self.weights["norm_w"], eps, x, x.shape[0],
+                          conv_state, ssm_state, out, self.workspace_q4(max(x.shape[0], 1)))
+        return out
 
     def block_weights(self, in_place: bool = False) -> Dict[str, Optional[torch.Tensor]]:
         """The parameters the block entry points take: w_in with the pre-norm's scale folded in
@@ -837,8 +1070,38 @@ class RomFfnMoe:
         self.w_down = conv(weights["w_down"], layer.tdtype)
         self.norm_w = conv(weights["norm_w"], torch.float32) if weights.get("norm_w") is not None else None
         self._packed: Dict[bool, torch.Tensor] = {}
+        self._q4: Dict[tuple, tuple] = {}
         self._ws: Optional[torch.Tensor] = None
+        self._step_ws: Optional[torch.Tensor] = None
         self._bwd_ws: Optional[torch.Tensor] = None
+
+    def q4_weights(self, group: int, pre_norm: bool):
+        """(gate | up in the library's row order, down), both in 4 bits, packed once."""
+        if (group, bool(pre_norm)) not in self._q4:
+            pack = lambda w: RomQ4Weight.pack(w, group).packed
+            self._q4[(group, bool(pre_norm))] = (pack(self.packed(bool(pre_norm))), pack(self.w_down))
+        return self._q4[(group, bool(pre_norm))]
+
+    def step(self, x: torch.Tensor, expert_idx: torch.Tensor, gate: torch.Tensor, pre_norm: bool = False, add_skip: bool = False,
+             q4_group: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The layer on up to ROM_FEW_TOKENS tokens x [N, d_model], straight from the routing decision expert_idx, gate
+        [N, K] (rom_ffn_moe_step); q4_group 32, 64 or 128: with the weights in 4 bits."""
+        n, d = x.shape[0], self.dims
+        out = torch.empty_like(x) if out is None else out
+        _on_current_device(x.device)
+        _expect(x, "x", self.w_down.dtype, (n, d.d_model), x.device)
+        _expect(out, "out", x.dtype, x.shape, x.device)
+        _expect(expert_idx, "expert_idx", torch.int32, (n, d.top_k), x.device)
+        _expect(gate, "gate", torch.float32, (n, d.top_k), x.device)
+        if self._step_ws is None:             # for ROM_FEW_TOKENS tokens: never replaced
+            need = rom_ffn_step_workspace_bytes(d, self.d_ff, ROM_FEW_TOKENS)
+            if need == 0:
+                raise RomError("rom_ffn_step_workspace_bytes returned 0: unsupported dims or d_ff")
+            self._step_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        gu, down = self.q4_weights(q4_group, pre_norm) if q4_group else (self.packed(bool(pre_norm)), self.w_down)
+        rom_ffn_moe_step(d, self.d_ff, gu, down, q4_group, pre_norm, self.eps, add_skip, x, n, expert_idx, gate, out,
+                         self._step_ws)
+        return out
 
     def packed(self, pre_norm: bool, drop_plain: bool = False) -> torch.Tensor:
         """w_gate_up in the library's packed row order, with the pre-norm's scale folded in or not."""
@@ -956,6 +1219,8 @@ class RomHybridStack:
                 self.ffn_structs[j] = _RomFfnWeights(_ptr(self._packed[j]), _ptr(f.w_down))
         self._tmp: Optional[torch.Tensor] = None
         self._ffn_ws: Optional[torch.Tensor] = None
+        self._q4: Dict[int, tuple] = {}
+        self._kept: list = []
 
     def forward(self, x: torch.Tensor, conv_state=None, ssm_state=None, return_states=False):
         B, L, _ = x.shape
@@ -974,6 +1239,48 @@ class RomHybridStack:
                                  B, L, conv_state, ssm_state, out, conv_out, ssm_out, self._tmp,
                                  self.layers[0].workspace(max(B, 1), max(L, 1)), self._ffn_ws)
         return (out, conv_out, ssm_out) if return_states else out
+
+    def quantize(self, group: int = 64) -> "RomHybridStack":
+        """Packs the projections and FFN weights of every layer in 4 bits for step(..., q4_group=group)."""
+        if group not in self._q4:
+            keep = [(ly.q4_weights(group, block=True), ly.weights["norm_w"]) for ly in self.layers]
+            structs = (_RomFfnWeights * len(self.ffns))()
+            ffn_keep = [None if f is None else f.q4_weights(group, self.ffn_pre_norm) for f in self.ffns]
+            for j, w in enumerate(ffn_keep):
+                if w is not None:
+                    structs[j] = _RomFfnWeights(_ptr(w[0]), _ptr(w[1]))
+            self._q4[group] = (make_blocks(keep), structs, keep, ffn_keep)
+        return self
+
+    def state_shapes(self, B: int):
+        n, d = len(self.layers), self.dims
+        return (n, B, d.d_inner, d.d_conv - 1), (n, B, d.d_inner, d.d_state)
+
+    def step(self, x: torch.Tensor, conv_state: torch.Tensor, ssm_state: torch.Tensor, q4_group: int = 0,
+             out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """One token per sequence, x [B, d_model], through the stack; states (state_shapes) in place.  q4_group: with the
+        4-bit weights of that group."""
+        B = x.shape[0]
+        out = torch.empty_like(x) if out is None else out
+        _on_current_device(x.device)
+        layer = self.layers[0]
+        _expect(x, "x", layer.tdtype, (B, self.dims.d_model), x.device)
+        _expect(out, "out", x.dtype, x.shape, x.device)
+        for t, what, shape in zip((conv_state, ssm_state), ("conv_state", "ssm_state"), self.state_shapes(B)):
+            _expect(t, what, torch.float32, shape, x.device)
+        if self._tmp is None or self._tmp.numel() != x.numel() or self._tmp.dtype != x.dtype:
+            self._tmp = torch.empty_like(x)
+        need = rom_hybrid_step_ffn_workspace_bytes(self.dims, self.d_ff, max(B, 1), q4_group)
+        if need == 0:
+            raise RomError("rom_hybrid_step_ffn_workspace_bytes returned 0: unsupported dims, d_ff, group or batch")
+        if self._ffn_ws is None or self._ffn_ws.numel() < need:
+            self._ffn_ws = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+        blocks, ffns = self.quantize(q4_group)._q4[q4_group][:2] if q4_group else (self.blocks, self.ffn_structs)
+        ws = layer.workspace_q4(max(B, 1)) if q4_group else layer.workspace(max(B, 1), 1)
+        _keep_if_captured(self._kept, self._tmp, self._ffn_ws, ws)
+        rom_hybrid_stack_step(self.dims, self.d_ff, blocks, ffns, q4_group, self.ffn_pre_norm, self.eps, x, B, conv_state,
+                              ssm_state, out, self._tmp, ws, self._ffn_ws)
+        return out
 
 
 class RomMamba2Layer:

@@ -265,10 +265,41 @@ int route_into(const rom_dims *d, const rom_weights *w, const void *x, int64_t n
   return ROM_OK;
 }
 
+// ---------------------------------------------------------------- a few tokens
+bool q4_group_ok(int group) { return group == 32 || group == 64 || group == 128; }
+
+// sizes of a stack of 4-bit matrices
+int check_q4(int32_t n_mats, int32_t rows, int32_t cols, int32_t group) {
+  if (n_mats <= 0 || rows <= 0 || cols <= 0 || !q4_group_ok(group)) return ROM_E_INVAL;
+  if (n_mats > kMaxExperts || rows % 8 != 0 || cols % 8 != 0 || rows > (1 << 20) || cols > (1 << 20)) return ROM_E_UNSUPPORTED;
+  // one thread per 16 bytes of codes, a grid of less than 2^32 threads
+  return q4_code_bytes(n_mats, rows, cols) <= (1ll << 33) ? ROM_OK : ROM_E_UNSUPPORTED;
+}
+
+size_t align_up(size_t bytes) { return (bytes + kAlign - 1) / kAlign * kAlign; }
+
+// what the projections of a step with 4-bit weights need behind the step's own plan
+size_t q4_step_scratch_bytes(const rom_dims *d, int64_t B) {
+  const size_t in = few_partial_bytes(2 * static_cast<int64_t>(d->d_inner), d->top_k, B), out = few_partial_bytes(d->d_model, d->top_k, B);
+  return align_up(in > out ? in : out);
+}
+
+// the checks of a step with 4-bit projections that come before forward_impl's
+int check_step_q4(const rom_dims *d, int32_t q4_group, int64_t B) {
+  const int rc = check_dims(d);
+  if (rc != ROM_OK) return rc;
+  if (!q4_group_ok(q4_group) || B < 0) return ROM_E_INVAL;
+  int q = check_q4(d->n_experts, 2 * d->d_inner, d->d_model, q4_group);
+  if (q == ROM_OK) q = check_q4(d->n_experts, d->d_model, d->d_inner, q4_group);
+  if (q != ROM_OK) return q;
+  return B <= ROM_FEW_TOKENS ? ROM_OK : ROM_E_UNSUPPORTED;
+}
+
 int forward_impl(const rom_dims *d, const rom_weights *w, const void *x, int64_t B, int64_t L,
                  const float *conv_in, const float *ssm_in, void *out, float *conv_out,
                  float *ssm_out, void *ws, size_t ws_bytes, hipStream_t s, const BlockOpts *blk = nullptr,
-                 const void *route_x = nullptr, const BlockOpts *route_blk = nullptr) {
+                 const void *route_x = nullptr, const BlockOpts *route_blk = nullptr, int q4_group = 0) {
+  // q4_group != 0 (a step): w_in and w_out are held in 4 bits with that group.
   // route_x / route_blk: the router alone reads route_x under route_blk's norm (the block's backward:
   // the decision of the forward block, which normalises x for itself, while everything else runs on
   // the materialised norm x)
@@ -284,7 +315,7 @@ int forward_impl(const rom_dims *d, const rom_weights *w, const void *x, int64_t
   if (B * L * d->top_k > (1ll << 30) || B > 65535) return ROM_E_UNSUPPORTED;
   const int64_t N = B * L;
   Plan p = make_plan(d, B, L);
-  if (ws_bytes < p.total) return ROM_E_WORKSPACE;
+  if (ws_bytes < p.total + (q4_group ? q4_step_scratch_bytes(d, N) : 0)) return ROM_E_WORKSPACE;
 
   char *base = static_cast<char *>(ws);
   auto at = [&](size_t off) { return base + off; };
@@ -337,8 +368,19 @@ int forward_impl(const rom_dims *d, const rom_weights *w, const void *x, int64_t
   ga.C = multi ? at(p.xz_sorted) : at(p.xz); ga.ldc = 2 * De; ga.c_rows = multi ? nullptr : tok_of_pos;
   // pre-norm block: x @ (W . norm_w)^T scaled by the token's 1/rms is RMSNorm(x) @ W^T
   if (!multi) ga.row_scale = rstd;
-  ROM_TRY(launch_grouped_gemm(ga, s));
-  if (multi)
+  FewArgs fa;
+  memset(&fa, 0, sizeof(fa));
+  fa.dtype = d->dtype; fa.group = q4_group; fa.n_mats = E; fa.N = static_cast<int>(N); fa.K = K;
+  fa.expert_idx = reinterpret_cast<const int32_t *>(at(p.expert_idx));
+  fa.partial = reinterpret_cast<float *>(at(p.total));
+  if (q4_group) {
+    fa.W = w->w_in; fa.rows = 2 * De; fa.cols = Dm;
+    fa.x = x; fa.row_scale = rstd; fa.out = at(p.xz);
+    ROM_TRY(launch_few(fa, s));
+  } else {
+    ROM_TRY(launch_grouped_gemm(ga, s));
+  }
+  if (multi && !q4_group)
     ROM_TRY(launch_slot_sum(eb == 4, eb == 4, at(p.xz_sorted), 2 * De, at(p.xz), 2 * De, inv_perm, N, K, 2 * De,
                             nullptr, 0, rstd, s));
   mark.end(ROM_STAGE_IN_PROJ, s);
@@ -440,6 +482,13 @@ int forward_impl(const rom_dims *d, const rom_weights *w, const void *x, int64_t
 
   // out projection, Eq. (13), and the gate-weighted combine, Eq. (12)
   mark.begin(ROM_STAGE_OUT_PROJ, s);
+  if (q4_group) {
+    fa.W = w->w_out; fa.rows = Dm; fa.cols = De;
+    fa.x = at(p.g); fa.gate = gate; fa.row_scale = nullptr; fa.residual = blk ? x : nullptr; fa.out = out;
+    ROM_TRY(launch_few(fa, s));
+    mark.end(ROM_STAGE_OUT_PROJ, s);
+    return ROM_OK;
+  }
   memset(&ga, 0, sizeof(ga));
   ga.dtype = d->dtype;
   ga.A = at(p.g); ga.lda = De; ga.a_rows = tok_of_pos; ga.a_span = N * De;
@@ -1208,6 +1257,219 @@ int rom_step_static(const rom_dims *dims, const rom_weights *w, const void *x, i
   // nothing in the step's workspace has to start at zero: every region is written before it is read
   return forward_impl(dims, w, x, B, 1, conv_state, ssm_state, out, conv_state, ssm_state, ws, kStaticScratchBytes,
                       static_cast<hipStream_t>(hip_stream));
+}
+
+// ---------------------------------------------------------------- a few tokens
+size_t rom_q4_bytes(int32_t n_mats, int32_t rows, int32_t cols, int32_t group) {
+  if (check_q4(n_mats, rows, cols, group) != ROM_OK) return 0;
+  const int64_t codes = q4_code_bytes(n_mats, rows, cols);
+  return static_cast<size_t>(codes + codes * 2 / group * 2);
+}
+
+namespace {
+int q4_convert_check(int dtype, const void *a, const void *b, int32_t n_mats, int32_t rows, int32_t cols, int32_t group) {
+  if (dtype != ROM_DTYPE_F32 && dtype != ROM_DTYPE_BF16) return ROM_E_INVAL;
+  const int rc = check_q4(n_mats, rows, cols, group);
+  if (rc != ROM_OK) return rc;
+  return a && b && a != b && aligned16(a) && aligned16(b) ? ROM_OK : ROM_E_INVAL;
+}
+}  // namespace
+
+int rom_q4_pack(int dtype, const void *w, int32_t n_mats, int32_t rows, int32_t cols, int32_t group, void *w_q4,
+                void *hip_stream) {
+  const int rc = q4_convert_check(dtype, w, w_q4, n_mats, rows, cols, group);
+  if (rc != ROM_OK) return rc;
+  ROM_TRY(launch_q4_pack(dtype, w, n_mats, rows, cols, group, w_q4, static_cast<hipStream_t>(hip_stream)));
+  return ROM_OK;
+}
+
+int rom_q4_unpack(int dtype, const void *w_q4, int32_t n_mats, int32_t rows, int32_t cols, int32_t group, void *w,
+                  void *hip_stream) {
+  const int rc = q4_convert_check(dtype, w_q4, w, n_mats, rows, cols, group);
+  if (rc != ROM_OK) return rc;
+  ROM_TRY(launch_q4_unpack(dtype, w_q4, n_mats, rows, cols, group, w, static_cast<hipStream_t>(hip_stream)));
+  return ROM_OK;
+}
+
+size_t rom_q4_project_workspace_bytes(int32_t rows, int32_t top_k, int64_t N) {
+  if (rows <= 0 || top_k < 1 || top_k > 8 || N < 0 || N > ROM_FEW_TOKENS) return 0;
+  return align_up(few_partial_bytes(rows, top_k, N));
+}
+
+int rom_q4_project(int dtype, const void *w_q4, int32_t n_mats, int32_t rows, int32_t cols, int32_t group, const void *x,
+                   int64_t N, int32_t top_k, const int32_t *expert_idx, const float *gate, const float *row_scale,
+                   const void *residual, void *out, void *ws, size_t ws_bytes, void *hip_stream) {
+  if (dtype != ROM_DTYPE_F32 && dtype != ROM_DTYPE_BF16) return ROM_E_INVAL;
+  const int rc = check_q4(n_mats, rows, cols, group);
+  if (rc != ROM_OK) return rc;
+  if (!w_q4 || !aligned16(w_q4) || N < 0 || top_k < 1) return ROM_E_INVAL;
+  if (!expert_idx && (n_mats != 1 || top_k != 1)) return ROM_E_INVAL;
+  if (top_k > 8 || N > ROM_FEW_TOKENS) return ROM_E_UNSUPPORTED;
+  if (N == 0) return ROM_OK;
+  if (!x || !out || x == out || !aligned16(x) || !aligned16(out) || (residual && !aligned16(residual))) return ROM_E_INVAL;
+  const size_t need = rom_q4_project_workspace_bytes(rows, top_k, N);
+  if (need && (!ws || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0)) return ROM_E_INVAL;
+  if (ws_bytes < need) return ROM_E_WORKSPACE;
+  FewArgs a;
+  memset(&a, 0, sizeof(a));
+  a.dtype = dtype; a.group = group; a.W = w_q4; a.n_mats = n_mats; a.rows = rows; a.cols = cols;
+  a.x = x; a.N = static_cast<int>(N); a.K = top_k; a.expert_idx = expert_idx;
+  a.gate = gate; a.row_scale = row_scale; a.residual = residual; a.out = out;
+  a.partial = static_cast<float *>(ws);
+  ROM_TRY(launch_few(a, static_cast<hipStream_t>(hip_stream)));
+  return ROM_OK;
+}
+
+namespace {
+int check_ffn_step(const rom_dims *d, int32_t d_ff, int32_t q4_group) {
+  int rc = check_ffn(d, d_ff);
+  if (rc != ROM_OK || q4_group == 0) return rc;
+  if (!q4_group_ok(q4_group)) return ROM_E_INVAL;
+  if (d_ff > (1 << 19)) return ROM_E_UNSUPPORTED;
+  rc = check_q4(d->n_experts, 2 * d_ff, d->d_model, q4_group);
+  return rc != ROM_OK ? rc : check_q4(d->n_experts, d->d_model, d_ff, q4_group);
+}
+struct FfnStepPlan {
+  size_t total, h, partial;
+};
+FfnStepPlan make_ffn_step_plan(const rom_dims *d, int32_t d_ff, int64_t N) {
+  FfnStepPlan p;
+  p.h = 0;
+  p.partial = align_up(static_cast<size_t>(N) * d->top_k * d_ff * (d->dtype == ROM_DTYPE_BF16 ? 2 : 4));
+  p.total = p.partial + align_up(few_partial_bytes(d->d_model, d->top_k, N));
+  return p;
+}
+}  // namespace
+
+size_t rom_ffn_step_workspace_bytes(const rom_dims *dims, int32_t d_ff, int64_t N) {
+  if (check_ffn(dims, d_ff) != ROM_OK || N < 0 || N > ROM_FEW_TOKENS) return 0;
+  return make_ffn_step_plan(dims, d_ff, N > 0 ? N : 1).total;
+}
+
+int rom_ffn_moe_step(const rom_dims *dims, int32_t d_ff, const rom_ffn_weights *w, int32_t q4_group, int pre_norm, float eps,
+                     int add_skip, const void *x, int64_t N, const int32_t *expert_idx, const float *gate, void *out, void *ws,
+                     size_t ws_bytes, void *hip_stream) {
+  const int rc = check_ffn_step(dims, d_ff, q4_group);
+  if (rc != ROM_OK) return rc;
+  if (!w || !w->w_gate_up || !w->w_down || !aligned16(w->w_gate_up) || !aligned16(w->w_down)) return ROM_E_INVAL;
+  if (N < 0 || (pre_norm && !(eps >= 0.0f))) return ROM_E_INVAL;
+  if (N > ROM_FEW_TOKENS) return ROM_E_UNSUPPORTED;
+  if (N == 0) return ROM_OK;
+  if (!x || !out || x == out || !expert_idx || !gate || !ws) return ROM_E_INVAL;
+  if (!aligned16(x) || !aligned16(out) || (reinterpret_cast<uintptr_t>(ws) % kAlign) != 0) return ROM_E_INVAL;
+  const FfnStepPlan p = make_ffn_step_plan(dims, d_ff, N);
+  if (ws_bytes < p.total) return ROM_E_WORKSPACE;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  char *base = static_cast<char *>(ws);
+  FewArgs a;
+  memset(&a, 0, sizeof(a));
+  a.dtype = dims->dtype; a.group = q4_group; a.n_mats = dims->n_experts;
+  a.N = static_cast<int>(N); a.K = dims->top_k; a.expert_idx = expert_idx;
+  a.W = w->w_gate_up; a.rows = 2 * d_ff; a.cols = dims->d_model;
+  a.x = x; a.norm = pre_norm ? 1 : 0; a.eps = eps; a.swiglu = 1; a.out = base + p.h;
+  ROM_TRY(launch_few(a, s));
+  a.W = w->w_down; a.rows = dims->d_model; a.cols = d_ff;
+  a.x = base + p.h; a.x_by_slot = 1; a.norm = 0; a.swiglu = 0;
+  a.gate = gate; a.residual = add_skip ? x : nullptr; a.out = out;
+  a.partial = reinterpret_cast<float *>(base + p.partial);
+  ROM_TRY(launch_few(a, s));
+  return ROM_OK;
+}
+
+size_t rom_step_q4_workspace_bytes(const rom_dims *dims, int64_t B) {
+  if (check_dims(dims) != ROM_OK || B < 0 || B > ROM_FEW_TOKENS) return 0;
+  const int64_t n = B > 0 ? B : 1;
+  return make_plan(dims, n, 1).total + q4_step_scratch_bytes(dims, n);
+}
+
+int rom_step_q4(const rom_dims *dims, const rom_weights *w, int32_t q4_group, const void *x, int64_t B, float *conv_state,
+                float *ssm_state, void *out, void *ws, size_t ws_bytes, void *hip_stream) {
+  const int rc = check_step_q4(dims, q4_group, B);
+  if (rc != ROM_OK) return rc;
+  if (B > 0 && (!conv_state || !ssm_state)) return ROM_E_INVAL;
+  return forward_impl(dims, w, x, B, 1, conv_state, ssm_state, out, conv_state, ssm_state, ws, ws_bytes,
+                      static_cast<hipStream_t>(hip_stream), nullptr, nullptr, nullptr, q4_group);
+}
+
+int rom_block_step_q4(const rom_dims *dims, const rom_weights *w, int32_t q4_group, const float *norm_weight, float eps,
+                      const void *x, int64_t B, float *conv_state, float *ssm_state, void *out, void *ws, size_t ws_bytes,
+                      void *hip_stream) {
+  const int rc = check_step_q4(dims, q4_group, B);
+  if (rc != ROM_OK) return rc;
+  if (B > 0 && (!conv_state || !ssm_state)) return ROM_E_INVAL;
+  const BlockOpts blk = {norm_weight, eps};
+  return forward_impl(dims, w, x, B, 1, conv_state, ssm_state, out, conv_state, ssm_state, ws, ws_bytes,
+                      static_cast<hipStream_t>(hip_stream), &blk, nullptr, nullptr, q4_group);
+}
+
+size_t rom_hybrid_step_ffn_workspace_bytes(const rom_dims *dims, int32_t d_ff, int64_t B, int32_t q4_group) {
+  if (check_ffn_step(dims, d_ff, q4_group) != ROM_OK || B < 0 || (q4_group && B > ROM_FEW_TOKENS)) return 0;
+  const int64_t n = B > 0 ? B : 1;
+  // room for a call is room for a smaller one: those of at most ROM_FEW_TOKENS run as rom_ffn_moe_step
+  const size_t few = make_ffn_step_plan(dims, d_ff, n < ROM_FEW_TOKENS ? n : ROM_FEW_TOKENS).total;
+  const size_t many = n > ROM_FEW_TOKENS ? make_ffn_plan(dims, d_ff, n).total : 0;
+  return few > many ? few : many;
+}
+
+int rom_hybrid_stack_step(const rom_dims *dims, int32_t d_ff, const rom_block *blocks, const rom_ffn_weights *ffns,
+                          int32_t q4_group, int ffn_pre_norm, int n_layers, float eps, const void *x, int64_t B,
+                          float *conv_state, float *ssm_state, void *out, void *tmp, void *ws, size_t ws_bytes, void *ffn_ws,
+                          size_t ffn_ws_bytes, void *hip_stream) {
+  int rc = check_ffn_step(dims, d_ff, q4_group);
+  if (rc != ROM_OK) return rc;
+  if (!blocks || !ffns || n_layers < 1 || B < 0 || !(eps >= 0.0f)) return ROM_E_INVAL;
+  if (q4_group && (rc = check_step_q4(dims, q4_group, B)) != ROM_OK) return rc;
+  int n_ops = 0;                        // RoM blocks plus the FFN-MoE blocks behind some of them
+  for (int j = 0; j < n_layers; ++j) {  // refuse the whole call before the first layer is launched
+    rc = check_weights(dims, &blocks[j].w);
+    if (rc != ROM_OK) return rc;
+    if (!blocks[j].norm_weight || !aligned16(blocks[j].norm_weight)) return ROM_E_INVAL;
+    n_ops += 1;
+    if (ffns[j].w_gate_up) {
+      if (!ffns[j].w_down || !aligned16(ffns[j].w_gate_up) || !aligned16(ffns[j].w_down)) return ROM_E_INVAL;
+      n_ops += 1;
+    }
+  }
+  const bool any_ffn = n_ops > n_layers;
+  if (n_ops > 1 && (!tmp || tmp == x || tmp == out || !aligned16(tmp))) return ROM_E_INVAL;
+  if (B == 0) return ROM_OK;
+  if (!x || !out || x == out || !conv_state || !ssm_state || !ws || (any_ffn && (!ffn_ws || ffn_ws == ws))) return ROM_E_INVAL;
+  if (any_ffn && (reinterpret_cast<uintptr_t>(ffn_ws) % kAlign) != 0) return ROM_E_INVAL;
+  if (B > 65535) return ROM_E_UNSUPPORTED;
+  const Plan p = make_plan(dims, B, 1);
+  if (any_ffn && ffn_ws_bytes < rom_hybrid_step_ffn_workspace_bytes(dims, d_ff, B, q4_group)) return ROM_E_WORKSPACE;
+  const size_t conv_per = static_cast<size_t>(B) * dims->d_inner * 3, ssm_per = static_cast<size_t>(B) * dims->d_inner * 16;
+  char *base = static_cast<char *>(ws);
+  const void *src = x;
+  int op = 0;
+  auto next_dst = [&]() {               // the blocks write out and tmp in turn, the last one out
+    void *dst = ((n_ops - 1 - op) & 1) ? tmp : out;
+    ++op;
+    return dst;
+  };
+  for (int j = 0; j < n_layers; ++j) {
+    void *dst = next_dst();
+    const BlockOpts blk = {blocks[j].norm_weight, eps};
+    rc = forward_impl(dims, &blocks[j].w, src, B, 1, conv_state + j * conv_per, ssm_state + j * ssm_per, dst,
+                      conv_state + j * conv_per, ssm_state + j * ssm_per, ws, ws_bytes, static_cast<hipStream_t>(hip_stream),
+                      &blk, nullptr, nullptr, q4_group);
+    if (rc != ROM_OK) return rc;
+    src = dst;
+    if (!ffns[j].w_gate_up) continue;
+    dst = next_dst();                   // the routing decision is where the RoM block has just left it
+    if (B <= ROM_FEW_TOKENS)
+      rc = rom_ffn_moe_step(dims, d_ff, &ffns[j], q4_group, ffn_pre_norm, eps, 1, src, B,
+                            reinterpret_cast<const int32_t *>(base + p.expert_idx), reinterpret_cast<const float *>(base + p.gate),
+                            dst, ffn_ws, ffn_ws_bytes, hip_stream);
+    else
+      rc = rom_ffn_moe_forward(dims, d_ff, &ffns[j], ffn_pre_norm, eps, 1, src, B,
+                               reinterpret_cast<const int32_t *>(base + p.offsets), reinterpret_cast<const int32_t *>(base + p.perm),
+                               reinterpret_cast<const int32_t *>(base + p.inv_perm), reinterpret_cast<const float *>(base + p.gate),
+                               dst, ffn_ws, ffn_ws_bytes, hip_stream);
+    if (rc != ROM_OK) return rc;
+    src = dst;
+  }
+  return ROM_OK;
 }
 
 // ---------------------------------------------------------------- RoM on a Mamba2 layer (Sec. 5.2, Table 3)

@@ -235,4 +235,34 @@ hipError_t launch_add(int dtype, const void *a, const void *b, void *dst, int64_
 hipError_t launch_ffn_prep(int dtype, const int32_t *perm, int top_k, int64_t n_slots, const void *x,
                            int d_model, float eps, int32_t *tok_of_pos, float *rstd_sorted, hipStream_t s);
 
+// ---------------------------------------------------------------- a few tokens (rom_few.hip)
+// Weights in 4 bits (E2M1 codes, bf16 scale per row and group of columns): layout in rom.h
+inline int64_t q4_pad_rows(int64_t rows) { return ceil_div(rows, 16) * 16; }
+inline int64_t q4_pad_cols(int64_t cols) { return ceil_div(cols, 128) * 128; }
+inline int64_t q4_code_bytes(int64_t n_mats, int64_t rows, int64_t cols) { return n_mats * q4_pad_rows(rows) * q4_pad_cols(cols) / 2; }
+hipError_t launch_q4_pack(int dtype, const void *w, int n_mats, int rows, int cols, int group, void *w_q4, hipStream_t s);
+hipError_t launch_q4_unpack(int dtype, const void *w_q4, int n_mats, int rows, int cols, int group, void *w, hipStream_t s);
+
+// One routed projection of S = N * K slots, slot s = n * K + k by matrix expert_idx[s] (NULL: matrix 0)
+struct FewArgs {
+  int dtype;                   // ROM_DTYPE_*: x, out, residual, plain weights
+  int group;                   // 0: W is T [n_mats, rows, cols]; else 4-bit weights with that group
+  const void *W;
+  int n_mats, rows, cols;
+  const void *x;               // T [N, cols], or [S, cols] with x_by_slot
+  int x_by_slot;
+  int N, K;
+  const int32_t *expert_idx;
+  int norm;                    // != 0: x / sqrt(mean(x^2) + eps) takes x's place
+  float eps;
+  int swiglu;                  // 1: rows are blocks of 8 gate + 8 up features; out T [S, rows / 2] = SiLU(gate) * up
+  // swiglu 0: out T [N, rows] = residual + row_scale * sum_k gate * (W x)
+  const float *gate, *row_scale;
+  const void *residual;
+  void *out;
+  float *partial;              // f32 of few_partial_bytes
+};
+size_t few_partial_bytes(int64_t rows, int K, int64_t N);
+hipError_t launch_few(const FewArgs &a, hipStream_t s);
+
 }  // namespace rom
