@@ -177,10 +177,17 @@ def routed_linear(inp, w, idx):
     out = np.zeros((inp.shape[0], w.shape[1]), F64)
     if n_exp == 1:
         return inp @ np.asarray(w[0], F64).T
+    # Some libraries add a row's products in an order that depends on how many rows are multiplied together: small
+    # ones are taken row by row, so that a token's bits do not depend on the others of its expert.
+    by_row = inp.shape[0] <= 256 and w.shape[1] * w.shape[2] <= 1 << 16
     for i in range(n_exp):
         rows = np.nonzero((idx == i).any(axis=1))[0]
-        if rows.size:
-            out[rows] += inp[rows] @ np.asarray(w[i], F64).T
+        wi = np.asarray(w[i], F64)
+        if by_row:
+            for r in rows:
+                out[r] += wi @ inp[r]
+        elif rows.size:
+            out[rows] += inp[rows] @ wi.T
     return out
 
 
