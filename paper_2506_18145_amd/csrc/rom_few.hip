@@ -5,22 +5,69 @@
 namespace rom {
 namespace {
 
-constexpr int kFewSlots = 8;
+constexpr int kFewSlots = 8;        // slots that one workgroup of few_slots_kernel meets together
 
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8_t;
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2_t;
+
+// ---------------------------------------------------------------- eight values of one lane
+// Eight neighbouring columns of a row, as the matrix instructions take them: lane (row or token l % 16, q = l / 16) holds
+// columns 8 q .. 8 q + 7 of a 32-wide step.
+template <typename T> struct Eight;
+
+template <> struct Eight<bf16_t> {
+  u32x4_t v;
+  __device__ __forceinline__ void load(const bf16_t *p) { v = *reinterpret_cast<const u32x4_t *>(p); }
+  __device__ __forceinline__ void zero_unless(bool ok) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = ok ? v[i] : 0u;
+  }
+  __device__ __forceinline__ float at(int i) const { return __uint_as_float(i & 1 ? v[i / 2] & 0xFFFF0000u : v[i / 2] << 16); }
+  // the eight E2M1 codes of a word: exact in bf16
+  __device__ __forceinline__ void codes(unsigned int w) {
+    v[0] = __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0));
+    v[1] = __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1));
+    v[2] = __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2));
+    v[3] = __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3));
+  }
+};
+
+template <> struct Eight<float> {
+  f32x4_t v[2];
+  __device__ __forceinline__ void load(const float *p) {
+    v[0] = reinterpret_cast<const f32x4_t *>(p)[0];
+    v[1] = reinterpret_cast<const f32x4_t *>(p)[1];
+  }
+  __device__ __forceinline__ void zero_unless(bool ok) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i / 4][i % 4] = ok ? v[i / 4][i % 4] : 0.0f;
+  }
+  __device__ __forceinline__ float at(int i) const { return v[i / 4][i % 4]; }
+  __device__ __forceinline__ void codes(unsigned int w) {
+    const f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
+    const f32x2_t c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
+    v[0] = f32x4_t{a[0], a[1], b[0], b[1]};
+    v[1] = f32x4_t{c[0], c[1], d[0], d[1]};
+  }
+};
+
+// D[row][col] += sum over the step's 32 columns of w[row] x[col]: lane (c, q) ends with rows 4 q .. 4 q + 3 of column c
+__device__ __forceinline__ f32x4_t mma(const Eight<bf16_t> &w, const Eight<bf16_t> &x, f32x4_t d) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w.v), __builtin_bit_cast(bf16x8_t, x.v), d, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4_t mma(const Eight<float> &w, const Eight<float> &x, f32x4_t d) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) d = __builtin_amdgcn_mfma_f32_16x16x4f32(w.at(i), x.at(i), d, 0, 0, 0);
+  return d;
+}
 
 // ---------------------------------------------------------------- weights in 4 bits
-// Byte `at` of a stack's codes: two neighbouring columns (low nibble first) of one row.
-struct Q4Place {
-  int64_t mat, row, col;       // col: of the low nibble
-};
-__device__ __forceinline__ Q4Place q4_place(int64_t at, int64_t row_tiles, int64_t col_blocks) {
-  const int64_t in_block = at & 1023, block = at >> 10;
-  const int q = static_cast<int>(in_block >> 8), r = static_cast<int>(in_block >> 4) & 15, j = static_cast<int>(in_block >> 2) & 3;
-  const int64_t tile = block / col_blocks;
-  return {tile / row_tiles, tile % row_tiles * 16 + r, block % col_blocks * 128 + 32 * j + 8 * q + 2 * (static_cast<int>(at) & 3)};
-}
+// A wavefront converts one block of 16 rows x 128 columns, a lane the 4 x 8 columns of its row that it will multiply: reads
+// of 64 bytes a row (two of them make a line), 1 KiB of codes in one piece.
 
 // the even code wins a tie: the midpoint above an even code belongs to it
 __device__ __forceinline__ unsigned int q4_code(float w, float s) {
@@ -30,177 +77,638 @@ __device__ __forceinline__ unsigned int q4_code(float w, float s) {
   return s > 0.0f && m > 0 ? m | (w < 0.0f ? 8u : 0u) : 0u;
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void q4_scale_kernel(const T *__restrict__ w, int n_mats, int rows, int cols, int group,
-                                                       bf16_t *__restrict__ scales) {
-  const int64_t row_tiles = (rows + 15) / 16, groups = (cols + 127) / 128 * (128 / group);
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= n_mats * row_tiles * groups * 16) return;
-  const int64_t tile = i / (groups * 16), mat = tile / row_tiles, row = tile % row_tiles * 16 + (i & 15), g = i / 16 % groups;
-  float top = 0.0f;
-  bool finite = true;
-  for (int c = 0; c < group; ++c) {
-    const int64_t col = g * group + c;
-    if (row >= rows || col >= cols) break;
-    const float v = fabsf(to_f32(w[(mat * rows + row) * cols + col]));
-    finite = finite && v < __builtin_inff();
-    top = fmaxf(top, v);
-  }
-  scales[i] = finite ? f32_to_bf16(top / 6.0f) : static_cast<bf16_t>(0x7FC0);
+struct Q4Block {
+  int64_t block, mat, row, scale;      // scale: index of group 0 of the block, row included
+  int col, r, q;                       // first column of the block
+  bool valid;
+};
+template <int G>
+__device__ __forceinline__ Q4Block q4_block(int n_mats, int rows, int cols) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row_tiles = (rows + 15) / 16, col_blocks = (cols + 127) / 128;
+  Q4Block b;
+  b.block = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  b.valid = b.block < n_mats * row_tiles * col_blocks;
+  const int64_t tile = b.block / col_blocks;
+  b.r = lane & 15;
+  b.q = lane >> 4;
+  b.mat = tile / row_tiles;
+  b.row = tile % row_tiles * 16 + b.r;
+  b.col = static_cast<int>(b.block % col_blocks) * 128;
+  b.scale = (tile * col_blocks + b.block % col_blocks) * (128 / G) * 16 + b.r;
+  return b;
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void q4_pack_kernel(const T *__restrict__ w, int n_mats, int rows, int cols, int group,
-                                                      const bf16_t *__restrict__ scales, unsigned char *__restrict__ codes) {
-  const int64_t row_tiles = (rows + 15) / 16, col_blocks = (cols + 127) / 128, groups = col_blocks * (128 / group);
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= n_mats * row_tiles * col_blocks * 1024) return;
-  const Q4Place p = q4_place(i, row_tiles, col_blocks);
-  unsigned int byte = 0;
-  if (p.row < rows && p.col < cols) {
-    const float s = bf16_to_f32(scales[((p.mat * row_tiles + p.row / 16) * groups + p.col / group) * 16 + p.row % 16]);
-    const T *at = w + (p.mat * rows + p.row) * cols + p.col;
-    byte = q4_code(to_f32(at[0]), s) | q4_code(to_f32(at[1]), s) << 4;
-  }
-  codes[i] = static_cast<unsigned char>(byte);
-}
-
-// value of the low code of byte `sel` of a word, of its high code
-__device__ __forceinline__ f32x2_t q4_pair(unsigned int word, int byte) {
-  return byte == 0   ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.0f, 0)
-         : byte == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.0f, 1)
-         : byte == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.0f, 2)
-                     : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, 1.0f, 3);
-}
-
-template <typename T>
-__global__ __launch_bounds__(256) void q4_unpack_kernel(const unsigned char *__restrict__ codes, const bf16_t *__restrict__ scales,
-                                                        int n_mats, int rows, int cols, int group, T *__restrict__ w) {
-  const int64_t row_tiles = (rows + 15) / 16, col_blocks = (cols + 127) / 128, groups = col_blocks * (128 / group);
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= n_mats * row_tiles * col_blocks * 1024) return;
-  const Q4Place p = q4_place(i, row_tiles, col_blocks);
-  if (p.row >= rows || p.col >= cols) return;
-  const float s = bf16_to_f32(scales[((p.mat * row_tiles + p.row / 16) * groups + p.col / group) * 16 + p.row % 16]);
-  const f32x2_t v = q4_pair(codes[i], 0);
-  T *at = w + (p.mat * rows + p.row) * cols + p.col;
-  at[0] = from_f32<T>(v[0] * s);
-  at[1] = from_f32<T>(v[1] * s);
-}
-
-// ---------------------------------------------------------------- routed projection
-__device__ __forceinline__ float wave_sum(float v) {
+template <typename T, int G>
+__global__ __launch_bounds__(256) void q4_pack_kernel(const T *__restrict__ w, int n_mats, int rows, int cols,
+                                                      unsigned char *__restrict__ codes, bf16_t *__restrict__ scales) {
+  const Q4Block b = q4_block<G>(n_mats, rows, cols);
+  if (!b.valid) return;
+  const T *src = w + (b.mat * rows + (b.row < rows ? b.row : 0)) * cols;
+  Eight<T> v[4];
 #pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m);
-  return v;
+  for (int j = 0; j < 4; ++j) {
+    const int k = b.col + 32 * j + 8 * b.q;
+    const bool ok = b.row < rows && k < cols;
+    v[j].load(src + (ok ? k : 0));
+    v[j].zero_unless(ok);
+  }
+  u32x4_t out;
+#pragma unroll
+  for (int g = 0; g < 128 / G; ++g) {
+    // the largest size over the group, infinity where something in it is not finite (a NaN does not pass fmaxf)
+    float top = 0.0f;
+#pragma unroll
+    for (int j = g * (G / 32); j < (g + 1) * (G / 32); ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float a = fabsf(v[j].at(i));
+        top = fmaxf(top, a < __builtin_inff() ? a : __builtin_inff());
+      }
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const bf16_t bits = top < __builtin_inff() ? f32_to_bf16(top / 6.0f) : static_cast<bf16_t>(0x7FC0);
+    const float s = bf16_to_f32(bits);
+#pragma unroll
+    for (int j = g * (G / 32); j < (g + 1) * (G / 32); ++j) {
+      unsigned int word = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) word |= q4_code(v[j].at(i), s) << (4 * i);
+      out[j] = word;
+    }
+    if (b.q == 0) scales[b.scale + g * 16] = bits;
+  }
+  *reinterpret_cast<u32x4_t *>(codes + b.block * 1024 + (b.q * 16 + b.r) * 16) = out;
 }
 
-// row `row` of matrix e times a row of x, this lane's share of the columns
-template <typename T>
-__device__ float few_dot(const FewArgs &a, int e, int row, const T *x, int lane) {
-  float sum = 0.0f;
-  if (a.group == 0) {
-    const T *w = static_cast<const T *>(a.W) + (static_cast<int64_t>(e) * a.rows + row) * a.cols;
-    for (int c = lane; c < a.cols; c += 64) sum = fmaf(to_f32(w[c]), to_f32(x[c]), sum);
-    return sum;
+template <typename T, int G>
+__global__ __launch_bounds__(256) void q4_unpack_kernel(const unsigned char *__restrict__ codes, const bf16_t *__restrict__ scales,
+                                                        int n_mats, int rows, int cols, T *__restrict__ w) {
+  const Q4Block b = q4_block<G>(n_mats, rows, cols);
+  if (!b.valid || b.row >= rows) return;
+  const u32x4_t in = *reinterpret_cast<const u32x4_t *>(codes + b.block * 1024 + (b.q * 16 + b.r) * 16);
+  T *dst = w + (b.mat * rows + b.row) * cols;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int k = b.col + 32 * j + 8 * b.q;
+    if (k >= cols) continue;
+    const float s = bf16_to_f32(scales[b.scale + j * 32 / G * 16]);
+    Eight<float> v;
+    v.codes(in[j]);
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) reinterpret_cast<f32x4_t *>(dst + k)[i] = f32x4_t{v.v[i][0] * s, v.v[i][1] * s, v.v[i][2] * s, v.v[i][3] * s};
+    } else {
+      u32x4_t o;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = pack_bf16x2(v.at(2 * i) * s, v.at(2 * i + 1) * s);
+      *reinterpret_cast<u32x4_t *>(dst + k) = o;
+    }
   }
-  const int64_t row_tiles = (a.rows + 15) / 16, col_blocks = (a.cols + 127) / 128, groups = col_blocks * (128 / a.group);
-  const int64_t tile = e * row_tiles + row / 16;
-  const unsigned char *codes = static_cast<const unsigned char *>(a.W);
-  const bf16_t *scales = reinterpret_cast<const bf16_t *>(codes + a.n_mats * row_tiles * col_blocks * 1024);
-  for (int c = 2 * lane; c < a.cols; c += 128) {
-    const int64_t at = (tile * col_blocks + c / 128) * 1024 + ((c % 32 / 8) * 16 + row % 16) * 16 + c % 128 / 32 * 4 + c % 8 / 2;
-    const f32x2_t v = q4_pair(codes[at], 0);
-    const float s = bf16_to_f32(scales[(tile * groups + c / a.group) * 16 + row % 16]);
-    sum = fmaf(s, v[0] * to_f32(x[c]) + v[1] * to_f32(x[c + 1]), sum);
+}
+
+// ---------------------------------------------------------------- routed projection, common parts
+// Where one expert's rows are read from.  G == 0: plain rows; else codes (blocks of a row tile lie together) and scales.
+template <typename T, int G>
+struct Matrix {
+  const T *plain;
+  const unsigned char *codes;
+  const bf16_t *scales;
+  int cols, col_blocks;
+
+  __device__ __forceinline__ Matrix(const FewArgs &a, int e) {
+    cols = a.cols;
+    col_blocks = (a.cols + 127) / 128;
+    if constexpr (G == 0) {
+      plain = static_cast<const T *>(a.W) + static_cast<int64_t>(e) * a.rows * a.cols;
+      codes = nullptr; scales = nullptr;
+    } else {
+      const int64_t tiles = (a.rows + 15) / 16;
+      plain = nullptr;
+      codes = static_cast<const unsigned char *>(a.W) + e * tiles * col_blocks * 1024;
+      scales = reinterpret_cast<const bf16_t *>(static_cast<const unsigned char *>(a.W) + a.n_mats * tiles * col_blocks * 1024) +
+               e * tiles * col_blocks * (128 / G) * 16;
+    }
   }
+  // 16 bytes of codes: row 16 tile + r, lane group q, block b
+  __device__ __forceinline__ u32x4_t words(int tile, int b, int q, int r) const {
+    return *reinterpret_cast<const u32x4_t *>(codes + (static_cast<int64_t>(tile) * col_blocks + b) * 1024 + (q * 16 + r) * 16);
+  }
+  // scales of rows 16 tile + r .. r + 3, group g of block b
+  __device__ __forceinline__ u32x2_t scale4(int tile, int b, int g, int r) const {
+    return *reinterpret_cast<const u32x2_t *>(scales + ((static_cast<int64_t>(tile) * col_blocks + b) * (128 / G) + g) * 16 + r);
+  }
+};
+
+__device__ __forceinline__ f32x4_t scaled_add(f32x4_t sum, f32x4_t d, u32x2_t s) {
+  sum[0] = fmaf(d[0], __uint_as_float(s[0] << 16), sum[0]);
+  sum[1] = fmaf(d[1], __uint_as_float(s[0] & 0xFFFF0000u), sum[1]);
+  sum[2] = fmaf(d[2], __uint_as_float(s[1] << 16), sum[2]);
+  sum[3] = fmaf(d[3], __uint_as_float(s[1] & 0xFFFF0000u), sum[3]);
   return sum;
 }
 
-// One wavefront per output value: the simplest form.
 template <typename T>
-__global__ __launch_bounds__(256) void few_plain_kernel(const FewArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int out_cols = a.swiglu ? a.rows / 2 : a.rows;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  const int64_t n_rows = a.swiglu ? static_cast<int64_t>(a.N) * a.K : a.N;
-  if (item >= n_rows * out_cols) return;
-  const int at = static_cast<int>(item / out_cols), col = static_cast<int>(item % out_cols);
-  const int n = a.swiglu ? at / a.K : at;
-  const T *xs = static_cast<const T *>(a.x);
-  float rstd = 1.0f;
-  if (a.norm) {
-    float sq = 0.0f;
-    for (int c = lane; c < a.cols; c += 64) {
-      const float v = to_f32(xs[static_cast<int64_t>(n) * a.cols + c]);
-      sq = fmaf(v, v, sq);
+__device__ __forceinline__ float square_sum(const Eight<T> &x, float sum) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sum = fmaf(x.at(i), x.at(i), sum);
+  return sum;
+}
+
+constexpr f32x4_t kZero4 = {0.0f, 0.0f, 0.0f, 0.0f};
+
+// a token's sum over its slots -> its output
+template <typename T>
+__device__ __forceinline__ void few_store(const FewArgs &a, int n, int row, float sum) {
+  const int64_t at = static_cast<int64_t>(n) * a.rows + row;
+  if (a.row_scale) sum *= a.row_scale[n];
+  if (a.residual) sum += to_f32(static_cast<const T *>(a.residual)[at]);
+  static_cast<T *>(a.out)[at] = from_f32<T>(sum);
+}
+
+// ---------------------------------------------------------------- up to eight slots
+// One pass over the picked experts' rows, bound by how many of their bytes are under way: a workgroup of eight wavefronts per
+// eight output rows, so that 2048 rows are a workgroup for every CU; the wavefronts deal the columns among
+// themselves, nothing but registers between a request and its product, and their sums meet in LDS.  The 16 x 16 matrix
+// instruction holds eight rows twice, columns 8 .. 15 of both operands being another part of the inner dimension:
+//   D[r][c] = first part,  D[8 + r][8 + c] = second part,  the other two quarters mean nothing.
+// A column is a slot, so that an expert that a token names twice is nothing special, and a slot never sees another's values.
+// Plain rows: the two parts are the halves of a 128-byte line (64 columns; 32 in fp32).  4 bits: neighbouring blocks.
+// SWIGLU: eight gate and eight up rows; blockIdx.y is a slot, its expert that of the first slot that names it.  Else with K
+// == 1 the same; with K > 1 a workgroup meets every expert in turn and adds a token's slots.
+template <typename T, int G, bool SWIGLU>
+__global__ __launch_bounds__(512) void few_slots_kernel(const FewArgs a) {
+  constexpr int RT = SWIGLU ? 2 : 1, WAVES = 8;
+  __shared__ __attribute__((aligned(16))) float red[WAVES][RT][2][8][8];    // wavefront, tile, part, slot, row
+  __shared__ float sq[WAVES][8];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int S = a.N * a.K;
+  const int row0 = blockIdx.x * (8 * RT);
+  int expert[kFewSlots];
+#pragma unroll
+  for (int i = 0; i < kFewSlots; ++i) {
+    const int e = i < S ? (a.expert_idx ? a.expert_idx[i] : 0) : -1;
+    expert[i] = e >= 0 && e < a.n_mats ? e : -1;
+  }
+  // bit s: slot s is the first that names its expert
+  unsigned int first = 0;
+#pragma unroll
+  for (int i = 0; i < kFewSlots; ++i) {
+    bool seen = expert[i] < 0;
+#pragma unroll
+    for (int j = 0; j < i; ++j) seen = seen || expert[j] == expert[i];
+    first |= seen ? 0u : 1u << i;
+  }
+  const bool by_slot = SWIGLU || a.K == 1;
+  const int y = blockIdx.y;
+  int mine = -1;                                                // by_slot: this workgroup's expert
+#pragma unroll
+  for (int i = 0; i < kFewSlots; ++i) mine = i == y ? expert[i] : mine;
+  if (by_slot) {
+    if (mine >= 0 && !((first >> y) & 1u)) return;              // another workgroup's
+    if (SWIGLU && mine < 0) return;
+    first &= 1u << y;
+  }
+
+  const int c = lane & 7, part = (lane >> 3) & 1, q = lane >> 4;      // operands: row or slot c, part, columns 8 q .. of a step
+  const int d_part = q >> 1, d_row = 4 * (q & 1);                     // result: rows d_row .. + 3 of part d_part, column lane & 15
+  int my_expert = -1;                                           // of slot c
+#pragma unroll
+  for (int i = 0; i < kFewSlots; ++i) my_expert = i == c ? expert[i] : my_expert;
+  const int x_slot = c < S ? c : S - 1;
+  const T *x = static_cast<const T *>(a.x) + static_cast<int64_t>(a.x_by_slot ? x_slot : x_slot / a.K) * a.cols;
+
+  f32x4_t total[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) total[t] = kZero4;
+  float squares = 0.0f;
+  for (unsigned int left = first; left; left &= left - 1) {
+    const int s = __builtin_ctz(left);
+    int e = -1;
+#pragma unroll
+    for (int i = 0; i < kFewSlots; ++i) e = i == s ? expert[i] : e;
+    const Matrix<T, G> m(a, e);
+    f32x4_t acc[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) acc[t] = kZero4;
+    if constexpr (G == 0) {
+      constexpr int UNITS = sizeof(T) == 2 ? 4 : 2;
+      const int units = (a.cols + 63) / 64;
+      for (int u0 = wave; u0 < units; u0 += WAVES * UNITS) {
+        Eight<T> w[UNITS][RT], v[UNITS];
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+          const int k = (u0 + i * WAVES) * 64 + 32 * part + 8 * q;
+          const int k_in = k < a.cols ? k : 0;
+#pragma unroll
+          for (int t = 0; t < RT; ++t) w[i][t].load(m.plain + static_cast<int64_t>(row0 + 8 * t + c) * a.cols + k_in);
+          v[i].load(x + k_in);
+        }
+        __builtin_amdgcn_sched_barrier(0);                      // all requests ahead of the first wait
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+          const bool ok = (u0 + i * WAVES) * 64 + 32 * part + 8 * q < a.cols;
+          v[i].zero_unless(ok);
+          if constexpr (SWIGLU) squares = square_sum(v[i], squares);
+#pragma unroll
+          for (int t = 0; t < RT; ++t) {
+            w[i][t].zero_unless(ok);
+            acc[t] = mma(w[i][t], v[i], acc[t]);
+          }
+        }
+      }
+    } else {
+      constexpr int UNITS = sizeof(T) == 2 ? 2 : 1, GROUPS = 128 / G;
+      const int units = (m.col_blocks + 1) / 2, tile = row0 / 16, r0 = row0 % 16;
+      for (int u0 = wave; u0 < units; u0 += WAVES * UNITS) {
+        u32x4_t w[UNITS][RT];
+        u32x2_t scale[UNITS][RT][GROUPS];
+        Eight<T> v[UNITS][4];
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+          const int b = 2 * (u0 + i * WAVES) + part, db = 2 * (u0 + i * WAVES) + d_part;
+          const int b_in = b < m.col_blocks ? b : 0, db_in = db < m.col_blocks ? db : 0;
+#pragma unroll
+          for (int t = 0; t < RT; ++t) {
+            w[i][t] = m.words(tile, b_in, q, r0 + 8 * t + c);
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) scale[i][t][g] = m.scale4(tile, db_in, g, r0 + 8 * t + d_row);
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int k = 128 * b + 32 * j + 8 * q;
+            v[i][j].load(x + (k < a.cols ? k : 0));
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+          const int b = 2 * (u0 + i * WAVES) + part;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            v[i][j].zero_unless(128 * b + 32 * j + 8 * q < a.cols);
+            if constexpr (SWIGLU) squares = square_sum(v[i][j], squares);
+          }
+#pragma unroll
+          for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+              f32x4_t d = kZero4;
+#pragma unroll
+              for (int j = g * (4 / GROUPS); j < (g + 1) * (4 / GROUPS); ++j) {
+                Eight<T> codes;
+                codes.codes(b < m.col_blocks ? w[i][t][j] : 0u);
+                d = mma(codes, v[i][j], d);
+              }
+              acc[t] = scaled_add(acc[t], d, scale[i][t][g]);
+            }
+        }
+      }
     }
-    rstd = 1.0f / sqrtf(wave_sum(sq) / a.cols + a.eps);
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) total[t][i] = my_expert == e ? acc[t][i] : total[t][i];
   }
-  T *out = static_cast<T *>(a.out) + item;
-  if (a.swiglu) {
-    const int e = a.expert_idx ? a.expert_idx[at] : 0;
-    if (e < 0 || e >= a.n_mats) return;
-    const T *x = xs + static_cast<int64_t>(n) * a.cols;
-    const float g = rstd * wave_sum(few_dot(a, e, col / 8 * 16 + col % 8, x, lane));
-    const float u = rstd * wave_sum(few_dot(a, e, col / 8 * 16 + col % 8 + 8, x, lane));
-    if (lane == 0) *out = from_f32<T>(g / (1.0f + expf(-g)) * u);
-    return;
+  if (part == d_part) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t) *reinterpret_cast<f32x4_t *>(&red[wave][t][part][c][d_row]) = total[t];
   }
+  if constexpr (SWIGLU) {
+    squares += __shfl_xor(squares, 8);
+    squares += __shfl_xor(squares, 16);
+    squares += __shfl_xor(squares, 32);
+    if (lane < 8) sq[wave][lane] = squares;
+  }
+  __syncthreads();
+  if (tid >= 64) return;
+  // thread (slot, row): the wavefronts' sums in wavefront order
+  const int slot = tid >> 3, r = tid & 7;
+  float v[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    v[t] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) v[t] += red[w][t][0][slot][r] + red[w][t][1][slot][r];
+  }
+  int slot_expert = -1;
+#pragma unroll
+  for (int i = 0; i < kFewSlots; ++i) slot_expert = i == slot ? expert[i] : slot_expert;
+  if constexpr (SWIGLU) {
+    if (slot >= S || slot_expert != mine) return;
+    float rstd = 1.0f;
+    if (a.norm) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) sum += sq[w][slot];
+      rstd = 1.0f / sqrtf(sum / a.cols + a.eps);
+    }
+    static_cast<T *>(a.out)[static_cast<int64_t>(slot) * (a.rows / 2) + row0 / 2 + r] = from_f32<T>(silu_f32(v[0] * rstd) * (v[1] * rstd));
+  } else {
+    float sum = v[0];
+    int n = slot;
+    if (a.K == 1) {
+      if (slot >= S || (mine >= 0 ? slot_expert != mine : slot != y)) return;
+      sum = mine >= 0 ? (a.gate ? a.gate[slot] * sum : sum) : 0.0f;
+    } else {
+      float weighted = slot_expert >= 0 ? (a.gate ? a.gate[slot] * sum : sum) : 0.0f;
+      sum = 0.0f;
+      for (int k = 0; k < a.K; ++k) {
+        const int src = (slot * a.K + k) * 8 + r;
+        sum += __shfl(weighted, src < 64 ? src : r);
+      }
+      if (n >= a.N) return;
+    }
+    few_store<T>(a, n, row0 + r, sum);
+  }
+}
+
+// ---------------------------------------------------------------- more slots
+// A workgroup owns RT row tiles of 16 for up to 16 TT slots of one expert; its wavefronts deal the blocks of 128
+// columns among themselves, and their sums meet in LDS.  Nothing has been sorted for it: every workgroup counts the slots of
+// each expert and finds the blockIdx.y-th piece (an expert and up to 16 TT of its slots) by itself.
+template <typename T, int G, bool SWIGLU, int RT, int TT>
+__global__ __launch_bounds__(256) void many_slots_kernel(const FewArgs a) {
+  constexpr int WAVES = 4, ROWS = 16 * RT, COLS = 16 * TT;
+  __shared__ __attribute__((aligned(16))) float red[WAVES][COLS][ROWS + 4];
+  __shared__ float sq[WAVES][COLS];
+  __shared__ int count[kMaxExperts];
+  __shared__ signed char slot_expert[ROM_FEW_TOKENS * 8];
+  __shared__ int slots[COLS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int S = a.N * a.K;
+  const int row0 = blockIdx.x * ROWS;
+  if (tid < kMaxExperts) count[tid] = 0;
+  __syncthreads();
+  for (int s = tid; s < S; s += 256) {
+    int e = a.expert_idx ? a.expert_idx[s] : 0;
+    e = e >= 0 && e < a.n_mats ? e : -1;
+    slot_expert[s] = static_cast<signed char>(e);
+    if (e >= 0) atomicAdd(&count[e], 1);
+  }
+  __syncthreads();
+  // lane = expert: its pieces, and how many lie before them
+  const int mine = count[lane], pieces = (mine + COLS - 1) / COLS;
+  int upto = pieces;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int v = __shfl_up(upto, d);
+    upto += lane >= d ? v : 0;
+  }
+  if constexpr (!SWIGLU) {
+    // slots that name no expert get the residual alone
+    if (a.K == 1 && blockIdx.y == 0) {
+      for (int s = 0; s < S; ++s)
+        if (slot_expert[s] < 0)
+          for (int r = tid; r < ROWS && row0 + r < a.rows; r += 256) few_store<T>(a, s, row0 + r, 0.0f);
+    }
+  }
+  const unsigned long long past = __ballot(upto > static_cast<int>(blockIdx.y));
+  if (past == 0) return;
+  const int e = __builtin_ctzll(past);
+  const int from = (static_cast<int>(blockIdx.y) - (__shfl(upto, e) - __shfl(pieces, e))) * COLS;
+  const int left = __shfl(mine, e) - from, n_cols = left < COLS ? left : COLS;
+  if (wave == 0) {
+    int seen = 0;
+    for (int s0 = 0; s0 < S && seen < from + n_cols; s0 += 64) {
+      const bool in = s0 + lane < S && slot_expert[s0 + lane] == e;
+      const unsigned long long b = __ballot(in);
+      const int at = seen + __popcll(b & ((1ull << lane) - 1)) - from;
+      if (in && at >= 0 && at < n_cols) slots[at] = s0 + lane;
+      seen += __popcll(b);
+    }
+  }
+  __syncthreads();
+
+  const int c = lane & 15, q = lane >> 4;
+  const Matrix<T, G> m(a, e);
+  const T *x[TT];
+#pragma unroll
+  for (int t = 0; t < TT; ++t) {
+    const int slot = slots[16 * t + c < n_cols ? 16 * t + c : 0];          // past the end: read again, not stored
+    x[t] = static_cast<const T *>(a.x) + static_cast<int64_t>(a.x_by_slot ? slot : slot / a.K) * a.cols;
+  }
+  f32x4_t acc[RT][TT];
+  float squares[TT];
+#pragma unroll
+  for (int t = 0; t < TT; ++t) {
+    squares[t] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < RT; ++i) acc[i][t] = kZero4;
+  }
+  for (int b = wave; b < m.col_blocks; b += WAVES) {
+    Eight<T> v[TT][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int k = 128 * b + 32 * j + 8 * q;
+#pragma unroll
+      for (int t = 0; t < TT; ++t) v[t][j].load(x[t] + (k < a.cols ? k : 0));
+    }
+    if constexpr (G == 0) {
+      Eight<T> w[RT][4];
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        const int row = row0 + 16 * i + c < a.rows ? row0 + 16 * i + c : 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int k = 128 * b + 32 * j + 8 * q;
+          w[i][j].load(m.plain + static_cast<int64_t>(row) * a.cols + (k < a.cols ? k : 0));
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool ok = 128 * b + 32 * j + 8 * q < a.cols;
+#pragma unroll
+        for (int t = 0; t < TT; ++t) v[t][j].zero_unless(ok);
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+          w[i][j].zero_unless(ok);
+#pragma unroll
+          for (int t = 0; t < TT; ++t) acc[i][t] = mma(w[i][j], v[t][j], acc[i][t]);
+        }
+      }
+    } else {
+      constexpr int GROUPS = 128 / G;
+      u32x4_t w[RT];
+      u32x2_t scale[RT][GROUPS];
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        const int tile = row0 + 16 * i < a.rows ? row0 / 16 + i : 0;
+        w[i] = m.words(tile, b, q, c);
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) scale[i][g] = m.scale4(tile, b, g, 4 * q);
+      }
+#pragma unroll
+      for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[t][j].zero_unless(128 * b + 32 * j + 8 * q < a.cols);
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+          f32x4_t d[TT];
+#pragma unroll
+          for (int t = 0; t < TT; ++t) d[t] = kZero4;
+#pragma unroll
+          for (int j = g * (4 / GROUPS); j < (g + 1) * (4 / GROUPS); ++j) {
+            Eight<T> codes;
+            codes.codes(w[i][j]);
+#pragma unroll
+            for (int t = 0; t < TT; ++t) d[t] = mma(codes, v[t][j], d[t]);
+          }
+#pragma unroll
+          for (int t = 0; t < TT; ++t) acc[i][t] = scaled_add(acc[i][t], d[t], scale[i][g]);
+        }
+    }
+    if constexpr (SWIGLU) {
+#pragma unroll
+      for (int t = 0; t < TT; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) squares[t] = square_sum(v[t][j], squares[t]);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < TT; ++t) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i) *reinterpret_cast<f32x4_t *>(&red[wave][16 * t + c][16 * i + 4 * q]) = acc[i][t];
+    if constexpr (SWIGLU) {
+      squares[t] += __shfl_xor(squares[t], 16);
+      squares[t] += __shfl_xor(squares[t], 32);
+      if (q == 0) sq[wave][16 * t + c] = squares[t];
+    }
+  }
+  __syncthreads();
+  const auto total = [&](int col, int r) __attribute__((always_inline)) {
+    float v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) v += red[w][col][r];
+    return v;
+  };
+  if constexpr (SWIGLU) {
+    for (int i = tid; i < n_cols * (ROWS / 2); i += 256) {
+      const int col = i / (ROWS / 2), f = i % (ROWS / 2), r = f / 8 * 16 + f % 8;
+      if (row0 + r >= a.rows) continue;
+      float rstd = 1.0f;
+      if (a.norm) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) sum += sq[w][col];
+        rstd = 1.0f / sqrtf(sum / a.cols + a.eps);
+      }
+      static_cast<T *>(a.out)[static_cast<int64_t>(slots[col]) * (a.rows / 2) + row0 / 2 + f] =
+          from_f32<T>(silu_f32(total(col, r) * rstd) * (total(col, r + 8) * rstd));
+    }
+  } else {
+    for (int i = tid; i < n_cols * ROWS; i += 256) {
+      const int col = i / ROWS, r = i % ROWS, slot = slots[col];
+      if (row0 + r >= a.rows) continue;
+      float v = total(col, r);
+      if (a.gate) v *= a.gate[slot];
+      if (a.K == 1) few_store<T>(a, slot, row0 + r, v);
+      else a.partial[static_cast<int64_t>(slot) * a.rows + row0 + r] = v;
+    }
+  }
+}
+
+// K > 1: a token's weighted slots, in slot order
+template <typename T>
+__global__ __launch_bounds__(256) void few_combine_kernel(const FewArgs a) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= static_cast<int64_t>(a.N) * a.rows) return;
+  const int n = static_cast<int>(i / a.rows), row = static_cast<int>(i % a.rows);
   float sum = 0.0f;
   for (int k = 0; k < a.K; ++k) {
-    const int64_t slot = static_cast<int64_t>(n) * a.K + k;
-    const int e = a.expert_idx ? a.expert_idx[slot] : 0;
-    if (e < 0 || e >= a.n_mats) continue;
-    const float v = wave_sum(few_dot(a, e, col, xs + (a.x_by_slot ? slot : n) * a.cols, lane));
-    sum = fmaf(a.gate ? a.gate[slot] : 1.0f, v, sum);
+    const int slot = n * a.K + k, e = a.expert_idx[slot];
+    if (e >= 0 && e < a.n_mats) sum += a.partial[static_cast<int64_t>(slot) * a.rows + row];
   }
-  if (a.row_scale) sum *= a.row_scale[n];
-  if (a.residual) sum += to_f32(static_cast<const T *>(a.residual)[item]);
-  if (lane == 0) *out = from_f32<T>(sum);
+  few_store<T>(a, n, row, sum);
 }
 
 unsigned blocks_of(int64_t n, int per) { return static_cast<unsigned>(ceil_div(n, per)); }
 
+template <typename T, int G>
+hipError_t convert(bool pack, const void *w, int n_mats, int rows, int cols, void *w_q4, hipStream_t s) {
+  unsigned char *codes = static_cast<unsigned char *>(w_q4);
+  const int64_t bytes = q4_code_bytes(n_mats, rows, cols);
+  bf16_t *scales = reinterpret_cast<bf16_t *>(codes + bytes);
+  const dim3 grid(blocks_of(bytes / 1024, 4)), block(256);
+  if (pack)
+    hipLaunchKernelGGL((q4_pack_kernel<T, G>), grid, block, 0, s, static_cast<const T *>(w), n_mats, rows, cols, codes, scales);
+  else
+    hipLaunchKernelGGL((q4_unpack_kernel<T, G>), grid, block, 0, s, codes, scales, n_mats, rows, cols,
+                       static_cast<T *>(const_cast<void *>(w)));
+  return hipGetLastError();
+}
+
 template <typename T>
-void pack_launches(const void *w, int n_mats, int rows, int cols, int group, unsigned char *codes, bf16_t *scales, hipStream_t s) {
-  const int64_t n_codes = q4_code_bytes(n_mats, rows, cols), n_scales = n_codes * 2 / group;
-  hipLaunchKernelGGL(q4_scale_kernel<T>, dim3(blocks_of(n_scales, 256)), dim3(256), 0, s, static_cast<const T *>(w), n_mats, rows,
-                     cols, group, scales);
-  hipLaunchKernelGGL(q4_pack_kernel<T>, dim3(blocks_of(n_codes, 256)), dim3(256), 0, s, static_cast<const T *>(w), n_mats, rows,
-                     cols, group, scales, codes);
+hipError_t convert_group(bool pack, const void *w, int n_mats, int rows, int cols, int group, void *w_q4, hipStream_t s) {
+  return group == 32   ? convert<T, 32>(pack, w, n_mats, rows, cols, w_q4, s)
+         : group == 64 ? convert<T, 64>(pack, w, n_mats, rows, cols, w_q4, s)
+                       : convert<T, 128>(pack, w, n_mats, rows, cols, w_q4, s);
+}
+
+template <typename T, int G, bool SWIGLU, int RT, int TT>
+void launch_many(const FewArgs &a, hipStream_t s) {
+  const int S = a.N * a.K;
+  // pieces: at most one that is not full for every expert met
+  const int pieces = (S < a.n_mats ? S : a.n_mats) + S / (16 * TT);
+  hipLaunchKernelGGL((many_slots_kernel<T, G, SWIGLU, RT, TT>), dim3(blocks_of(a.rows, 16 * RT), pieces), dim3(256), 0, s, a);
+}
+
+template <typename T, int G, bool SWIGLU>
+hipError_t launch_form(const FewArgs &a, hipStream_t s) {
+  const int S = a.N * a.K;
+  if (S <= kFewSlots) {
+    hipLaunchKernelGGL((few_slots_kernel<T, G, SWIGLU>), dim3(a.rows / (SWIGLU ? 16 : 8), SWIGLU || a.K == 1 ? S : 1), dim3(512), 0, s, a);
+    return hipGetLastError();
+  }
+  if constexpr (sizeof(T) == 4) {
+    launch_many<T, G, SWIGLU, 1, 1>(a, s);
+  } else {
+    const int64_t met = S < a.n_mats ? S : a.n_mats;
+    const bool narrow = S <= 8 * met;
+    if (a.rows / 64 * met >= 512) {
+      if (narrow) launch_many<T, G, SWIGLU, 4, 1>(a, s);
+      else launch_many<T, G, SWIGLU, 4, 2>(a, s);
+    } else {
+      if (narrow) launch_many<T, G, SWIGLU, 2, 1>(a, s);
+      else launch_many<T, G, SWIGLU, 2, 2>(a, s);
+    }
+  }
+  if (!SWIGLU && a.K > 1)
+    hipLaunchKernelGGL(few_combine_kernel<T>, dim3(blocks_of(static_cast<int64_t>(a.N) * a.rows, 256)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <typename T, bool SWIGLU>
+hipError_t launch_group(const FewArgs &a, hipStream_t s) {
+  switch (a.group) {
+    case 0: return launch_form<T, 0, SWIGLU>(a, s);
+    case 32: return launch_form<T, 32, SWIGLU>(a, s);
+    case 64: return launch_form<T, 64, SWIGLU>(a, s);
+    default: return launch_form<T, 128, SWIGLU>(a, s);
+  }
 }
 
 }  // namespace
 
 hipError_t launch_q4_pack(int dtype, const void *w, int n_mats, int rows, int cols, int group, void *w_q4, hipStream_t s) {
-  unsigned char *codes = static_cast<unsigned char *>(w_q4);
-  bf16_t *scales = reinterpret_cast<bf16_t *>(codes + q4_code_bytes(n_mats, rows, cols));
-  if (dtype == ROM_DTYPE_BF16) pack_launches<bf16_t>(w, n_mats, rows, cols, group, codes, scales, s);
-  else pack_launches<float>(w, n_mats, rows, cols, group, codes, scales, s);
-  return hipGetLastError();
+  return dtype == ROM_DTYPE_BF16 ? convert_group<bf16_t>(true, w, n_mats, rows, cols, group, w_q4, s)
+                                 : convert_group<float>(true, w, n_mats, rows, cols, group, w_q4, s);
 }
 
 hipError_t launch_q4_unpack(int dtype, const void *w_q4, int n_mats, int rows, int cols, int group, void *w, hipStream_t s) {
-  const unsigned char *codes = static_cast<const unsigned char *>(w_q4);
-  const int64_t n = q4_code_bytes(n_mats, rows, cols);
-  const bf16_t *scales = reinterpret_cast<const bf16_t *>(codes + n);
-  const dim3 grid(blocks_of(n, 256)), block(256);
-  if (dtype == ROM_DTYPE_BF16)
-    hipLaunchKernelGGL(q4_unpack_kernel<bf16_t>, grid, block, 0, s, codes, scales, n_mats, rows, cols, group, static_cast<bf16_t *>(w));
-  else
-    hipLaunchKernelGGL(q4_unpack_kernel<float>, grid, block, 0, s, codes, scales, n_mats, rows, cols, group, static_cast<float *>(w));
-  return hipGetLastError();
+  void *q = const_cast<void *>(w_q4);
+  return dtype == ROM_DTYPE_BF16 ? convert_group<bf16_t>(false, w, n_mats, rows, cols, group, q, s)
+                                 : convert_group<float>(false, w, n_mats, rows, cols, group, q, s);
 }
 
 // a slot's products where a token has several slots and the call is too large for one workgroup to meet them all
 size_t few_partial_bytes(int64_t rows, int K, int64_t N) { return K > 1 && N * K > kFewSlots ? static_cast<size_t>(N * K * rows) * 4 : 0; }
 
 hipError_t launch_few(const FewArgs &a, hipStream_t s) {
-  const int64_t items = (a.swiglu ? static_cast<int64_t>(a.N) * a.K * (a.rows / 2) : static_cast<int64_t>(a.N) * a.rows);
-  if (a.dtype == ROM_DTYPE_BF16) hipLaunchKernelGGL(few_plain_kernel<bf16_t>, dim3(blocks_of(items, 4)), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(few_plain_kernel<float>, dim3(blocks_of(items, 4)), dim3(256), 0, s, a);
-  return hipGetLastError();
+  if (a.dtype == ROM_DTYPE_BF16) return a.swiglu ? launch_group<bf16_t, true>(a, s) : launch_group<bf16_t, false>(a, s);
+  return a.swiglu ? launch_group<float, true>(a, s) : launch_group<float, false>(a, s);
 }
 
 }  // namespace rom
