@@ -576,25 +576,37 @@ def rom_probe(kind: int, p0: int, p1: int, n_blocks: int, iters: int, scratch: t
 ROM_FEW_TOKENS = 256
 
 
-def _expect(t: Optional[torch.Tensor], what: str, dtype, shape, device) -> None:
+def _expect(t: Optional[torch.Tensor], what: str, dtype, shape, index: int) -> None:
     """Type, shape, layout and device of a tensor that a kernel is about to read or write through its pointer."""
-    if t is None:
-        return
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
-        raise RomError(f"{what}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype} "
-                       f"{tuple(t.shape)} on {t.device}")
+    if t is not None and (t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous()):
+        raise RomError(f"{what}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{index}, got {t.dtype} "
+                       f"{tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
 
 
-def _on_current_device(device) -> None:
-    """The calls go to the current device's current stream."""
-    if device.type != "cuda" or (device.index is not None and device.index != torch.cuda.current_device()):
-        raise RomError(f"tensors on {device}, which is not the current device")
+def _current_index(t: torch.Tensor) -> int:
+    """Index of t's device, which has to be the current one: the calls go to its current stream."""
+    index = t.get_device()
+    if index < 0 or index != torch.cuda.current_device():
+        raise RomError(f"a tensor on {t.device}, which is not the current device")
+    return index
+
+
+# the current stream's handle without the Stream object around it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _at(t: Optional[torch.Tensor]) -> Optional[int]:
+    """Address of a tensor that _expect has seen."""
+    return None if t is None else t.data_ptr()
 
 
 def _keep_if_captured(kept: list, *buffers) -> None:
     """A buffer that a captured call uses has to outlive the holder's next, larger one: the graph goes on using it."""
     if torch.cuda.is_current_stream_capturing():
         kept.extend(b for b in buffers if b is not None and not any(b is k for k in kept))
+
+
+_TORCH_TYPE = {ROM_DTYPE_F32: torch.float32, ROM_DTYPE_BF16: torch.bfloat16}
 
 
 def _dtype_code(dtype) -> int:
@@ -612,17 +624,20 @@ def rom_q4_bytes(n_mats: int, rows: int, cols: int, group: int) -> int:
 def rom_q4_pack(w: torch.Tensor, group: int, w_q4: torch.Tensor) -> None:
     """w [n_mats, rows, cols] -> w_q4 uint8 [rom_q4_bytes(...)]"""
     n, rows, cols = w.shape
-    _on_current_device(w.device)
-    _expect(w_q4, "w_q4", torch.uint8, (rom_q4_bytes(n, rows, cols, group),), w.device)
-    _check(load_library().rom_q4_pack(_dtype_code(w.dtype), _ptr(w), n, rows, cols, group, _ptr(w_q4), _stream()), "rom_q4_pack")
+    index = _current_index(w)
+    _expect(w, "w", w.dtype, w.shape, index)
+    _expect(w_q4, "w_q4", torch.uint8, (rom_q4_bytes(n, rows, cols, group),), index)
+    _check(load_library().rom_q4_pack(_dtype_code(w.dtype), _at(w), n, rows, cols, group, _at(w_q4), _raw_stream(index)),
+           "rom_q4_pack")
 
 
 def rom_q4_unpack(w_q4: torch.Tensor, group: int, w: torch.Tensor) -> None:
     """w_q4 -> w [n_mats, rows, cols], the values that the codes stand for"""
     n, rows, cols = w.shape
-    _on_current_device(w.device)
-    _expect(w_q4, "w_q4", torch.uint8, (rom_q4_bytes(n, rows, cols, group),), w.device)
-    _check(load_library().rom_q4_unpack(_dtype_code(w.dtype), _ptr(w_q4), n, rows, cols, group, _ptr(w), _stream()),
+    index = _current_index(w)
+    _expect(w, "w", w.dtype, w.shape, index)
+    _expect(w_q4, "w_q4", torch.uint8, (rom_q4_bytes(n, rows, cols, group),), index)
+    _check(load_library().rom_q4_unpack(_dtype_code(w.dtype), _at(w_q4), n, rows, cols, group, _at(w), _raw_stream(index)),
            "rom_q4_unpack")
 
 
@@ -630,11 +645,21 @@ def rom_q4_project_workspace_bytes(rows: int, top_k: int, n_tokens: int) -> int:
     return int(load_library().rom_q4_project_workspace_bytes(rows, top_k, n_tokens))
 
 
-def rom_q4_project(dtype, w_q4, n_mats, rows, cols, group, x, n_tokens, top_k, expert_idx, gate, row_scale, residual, out, ws):
+def rom_q4_project(w_q4, n_mats, rows, cols, group, x, expert_idx, gate, row_scale, residual, out, ws):
+    """x [N, cols], out [N, rows]; top_k is expert_idx's second size (1 without)."""
+    index = _current_index(x)
+    n, k, dtype = x.shape[0], 1 if expert_idx is None else expert_idx.shape[-1], x.dtype
+    _expect(x, "x", dtype, (n, cols), index)
+    _expect(expert_idx, "expert_idx", torch.int32, (n, k), index)
+    _expect(gate, "gate", torch.float32, (n, k), index)
+    _expect(row_scale, "row_scale", torch.float32, (n,), index)
+    _expect(residual, "residual", dtype, (n, rows), index)
+    _expect(out, "out", dtype, (n, rows), index)
     code = load_library().rom_q4_project(
-        dtype, _ptr(w_q4), n_mats, rows, cols, group, _ptr(x), n_tokens, top_k, _ptr(expert_idx), _ptr(gate),
-        _ptr(row_scale), _ptr(residual), _ptr(out), _ptr(ws), _nbytes(ws), _stream())
-    _check(code, "rom_q4_project")
+        _dtype_code(dtype), w_q4.data_ptr(), n_mats, rows, cols, group, x.data_ptr(), n, k, _at(expert_idx), _at(gate),
+        _at(row_scale), _at(residual), out.data_ptr(), _at(ws), _nbytes(ws), _raw_stream(index))
+    if code:
+        _check(code, "rom_q4_project")
 
 
 def rom_ffn_step_workspace_bytes(dims, d_ff: int, n_tokens: int) -> int:
@@ -642,11 +667,17 @@ def rom_ffn_step_workspace_bytes(dims, d_ff: int, n_tokens: int) -> int:
 
 
 def rom_ffn_moe_step(dims, d_ff, w_gate_up, w_down, q4_group, pre_norm, eps, add_skip, x, n_tokens, expert_idx, gate, out, ws):
-    w = _RomFfnWeights(_ptr(w_gate_up), _ptr(w_down))
+    index, k, dtype = _current_index(x), dims.top_k, _TORCH_TYPE.get(dims.dtype)
+    _expect(x, "x", dtype, (n_tokens, dims.d_model), index)
+    _expect(out, "out", dtype, (n_tokens, dims.d_model), index)
+    _expect(expert_idx, "expert_idx", torch.int32, (n_tokens, k), index)
+    _expect(gate, "gate", torch.float32, (n_tokens, k), index)
+    w = _RomFfnWeights(w_gate_up.data_ptr(), w_down.data_ptr())
     code = load_library().rom_ffn_moe_step(
-        ctypes.byref(dims), d_ff, ctypes.byref(w), q4_group, int(bool(pre_norm)), eps, int(bool(add_skip)), _ptr(x),
-        n_tokens, _ptr(expert_idx), _ptr(gate), _ptr(out), _ptr(ws), _nbytes(ws), _stream())
-    _check(code, "rom_ffn_moe_step")
+        ctypes.byref(dims), d_ff, ctypes.byref(w), q4_group, 1 if pre_norm else 0, eps, 1 if add_skip else 0, x.data_ptr(),
+        n_tokens, expert_idx.data_ptr(), gate.data_ptr(), out.data_ptr(), ws.data_ptr(), _nbytes(ws), _raw_stream(index))
+    if code:
+        _check(code, "rom_ffn_moe_step")
 
 
 def rom_step_q4_workspace_bytes(dims, B: int) -> int:
@@ -688,18 +719,20 @@ class RomQ4Weight:
         need = rom_q4_bytes(n_mats, rows, cols, group)
         if need == 0:
             raise RomError(f"rom_q4_bytes returned 0: unsupported sizes [{n_mats}, {rows}, {cols}] in groups of {group}")
-        _expect(packed, "packed", torch.uint8, (need,), packed.device)
+        if packed.device.type != "cuda":
+            raise RomError("RomQ4Weight needs a GPU: librom has no CPU path")
+        self.index = packed.get_device()
+        _expect(packed, "packed", torch.uint8, (need,), self.index)
         self.packed, self.n_mats, self.rows, self.cols, self.group = packed, n_mats, rows, cols, group
         self.device = packed.device
-        self._ws: Dict[int, torch.Tensor] = {}      # by top_k, for ROM_FEW_TOKENS tokens: never replaced
+        self._ws: Dict[int, Optional[torch.Tensor]] = {}      # by top_k, for ROM_FEW_TOKENS tokens: never replaced
 
     @classmethod
     def pack(cls, w: torch.Tensor, group: int = 64) -> "RomQ4Weight":
         """w: bf16 or fp32, [n_mats, rows, cols] or one matrix [rows, cols]."""
         w = w.unsqueeze(0) if w.dim() == 2 else w
-        packed = torch.empty(rom_q4_bytes(*w.shape, group), dtype=torch.uint8, device=w.device)
-        out = cls(packed, *w.shape, group)
-        rom_q4_pack(w, group, packed)
+        out = cls(torch.empty(rom_q4_bytes(*w.shape, group), dtype=torch.uint8, device=w.device), *w.shape, group)
+        rom_q4_pack(w, group, out.packed)
         return out
 
     def unpack(self, dtype=torch.bfloat16) -> torch.Tensor:
@@ -711,21 +744,16 @@ class RomQ4Weight:
                 row_scale: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """residual + row_scale * sum_k gate[:, k] * (W[expert_idx[:, k]] x) for x [N, cols] (rom_q4_project)."""
-        n, k = x.shape[0], expert_idx.shape[1] if expert_idx is not None else 1
+        k = 1 if expert_idx is None else expert_idx.shape[-1]
         if out is None:
-            out = torch.empty((n, self.rows), dtype=x.dtype, device=x.device)
-        _on_current_device(self.device)
-        _expect(x, "x", x.dtype, (n, self.cols), self.device)
-        _expect(expert_idx, "expert_idx", torch.int32, (n, k), self.device)
-        _expect(gate, "gate", torch.float32, (n, k), self.device)
-        _expect(row_scale, "row_scale", torch.float32, (n,), self.device)
-        _expect(residual, "residual", x.dtype, (n, self.rows), self.device)
-        _expect(out, "out", x.dtype, (n, self.rows), self.device)
+            out = torch.empty((x.shape[0], self.rows), dtype=x.dtype, device=x.device)
+        if x.get_device() != self.index:
+            raise RomError(f"x on {x.device}, the weights on {self.device}")
         if k not in self._ws:
-            self._ws[k] = torch.empty(rom_q4_project_workspace_bytes(self.rows, k, ROM_FEW_TOKENS), dtype=torch.uint8,
-                                      device=self.device)
-        rom_q4_project(_dtype_code(x.dtype), self.packed, self.n_mats, self.rows, self.cols, self.group, x, n, k, expert_idx,
-                       gate, row_scale, residual, out, self._ws[k])
+            need = rom_q4_project_workspace_bytes(self.rows, k, ROM_FEW_TOKENS)
+            self._ws[k] = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+        rom_q4_project(self.packed, self.n_mats, self.rows, self.cols, self.group, x, expert_idx, gate, row_scale, residual, out,
+                       self._ws[k])
         return out
 
 
@@ -780,12 +808,11 @@ class RomLayer:
         return self._ws
 
     def _check_step(self, x, conv_state, ssm_state, out):
-        B, d = x.shape[0], self.dims
-        _on_current_device(x.device)
-        _expect(x, "x", self.tdtype, (B, d.d_model), x.device)
-        _expect(out, "out", self.tdtype, (B, d.d_model), x.device)
-        _expect(conv_state, "conv_state", torch.float32, (B, d.d_inner, d.d_conv - 1), x.device)
-        _expect(ssm_state, "ssm_state", torch.float32, (B, d.d_inner, d.d_state), x.device)
+        B, d, index = x.shape[0], self.dims, _current_index(x)
+        _expect(x, "x", self.tdtype, (B, d.d_model), index)
+        _expect(out, "out", self.tdtype, (B, d.d_model), index)
+        _expect(conv_state, "conv_state", torch.float32, (B, d.d_inner, d.d_conv - 1), index)
+        _expect(ssm_state, "ssm_state", torch.float32, (B, d.d_inner, d.d_state), index)
 
     def step_q4(self, x: torch.Tensor, conv_state: torch.Tensor, ssm_state: torch.Tensor, group: int = 64,
                 out: Optional[torch.Tensor] = None):
@@ -1088,11 +1115,6 @@ class RomFfnMoe:
         [N, K] (rom_ffn_moe_step); q4_group 32, 64 or 128: with the weights in 4 bits."""
         n, d = x.shape[0], self.dims
         out = torch.empty_like(x) if out is None else out
-        _on_current_device(x.device)
-        _expect(x, "x", self.w_down.dtype, (n, d.d_model), x.device)
-        _expect(out, "out", x.dtype, x.shape, x.device)
-        _expect(expert_idx, "expert_idx", torch.int32, (n, d.top_k), x.device)
-        _expect(gate, "gate", torch.float32, (n, d.top_k), x.device)
         if self._step_ws is None:             # for ROM_FEW_TOKENS tokens: never replaced
             need = rom_ffn_step_workspace_bytes(d, self.d_ff, ROM_FEW_TOKENS)
             if need == 0:
@@ -1262,12 +1284,11 @@ class RomHybridStack:
         4-bit weights of that group."""
         B = x.shape[0]
         out = torch.empty_like(x) if out is None else out
-        _on_current_device(x.device)
-        layer = self.layers[0]
-        _expect(x, "x", layer.tdtype, (B, self.dims.d_model), x.device)
-        _expect(out, "out", x.dtype, x.shape, x.device)
+        layer, index = self.layers[0], _current_index(x)
+        _expect(x, "x", layer.tdtype, (B, self.dims.d_model), index)
+        _expect(out, "out", x.dtype, x.shape, index)
         for t, what, shape in zip((conv_state, ssm_state), ("conv_state", "ssm_state"), self.state_shapes(B)):
-            _expect(t, what, torch.float32, shape, x.device)
+            _expect(t, what, torch.float32, shape, index)
         if self._tmp is None or self._tmp.numel() != x.numel() or self._tmp.dtype != x.dtype:
             self._tmp = torch.empty_like(x)
         need = rom_hybrid_step_ffn_workspace_bytes(self.dims, self.d_ff, max(B, 1), q4_group)

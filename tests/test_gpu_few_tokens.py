@@ -114,8 +114,7 @@ def check_project(q, values, x, idx, gate, row_scale, residual, dtype):
     out = torch.full((N, q.rows), float("nan"), dtype=TYPES[dtype], device=DEV)
     ws_bytes = rom_q4_project_workspace_bytes(q.rows, K, N)
     whole, ws = guarded(max(ws_bytes, 256))
-    rom_q4_project(1 if dtype == "bf16" else 0, q.packed, q.n_mats, q.rows, q.cols, q.group, x, N, K, idx, gate, row_scale,
-                   residual, out, ws)
+    rom_q4_project(q.packed, q.n_mats, q.rows, q.cols, q.group, x, idx, gate, row_scale, residual, out, ws)
     want, size = F.project(np64(x), values, idx.cpu().numpy(), None if gate is None else np64(gate),
                            None if row_scale is None else np64(row_scale), None if residual is None else np64(residual))
     tol = unit(dtype) * np.abs(want) * 1.001 + (q.cols + 64) * 2.0 ** -24 * size + 2.0 ** -24 * np.abs(want)
