@@ -194,17 +194,34 @@ struct Matrix {
   __device__ __forceinline__ u32x4_t words(int tile, int b, int q, int r) const {
     return *reinterpret_cast<const u32x4_t *>(codes + (static_cast<int64_t>(tile) * col_blocks + b) * 1024 + (q * 16 + r) * 16);
   }
-  // scales of rows 16 tile + r .. r + 3, group g of block b
-  __device__ __forceinline__ u32x2_t scale4(int tile, int b, int g, int r) const {
+  // scales of rows 16 tile + r .. r + 3 in block b: the lanes of a quad hold its groups
+  __device__ __forceinline__ u32x2_t scale4(int tile, int b, int r) const {
+    const int g = static_cast<int>(threadIdx.x) & (128 / G - 1);
     return *reinterpret_cast<const u32x2_t *>(scales + ((static_cast<int64_t>(tile) * col_blocks + b) * (128 / G) + g) * 16 + r);
   }
 };
 
+// what lane g of every quad holds
+template <int g>
+__device__ __forceinline__ u32x2_t quad_lane(u32x2_t v) {
+  u32x2_t o;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    o[i] = static_cast<unsigned int>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v[i]), g * 0x55, 0xF, 0xF, true));
+  return o;
+}
+__device__ __forceinline__ u32x2_t quad_lane(u32x2_t v, int g) {
+  return g == 0 ? quad_lane<0>(v) : g == 1 ? quad_lane<1>(v) : g == 2 ? quad_lane<2>(v) : quad_lane<3>(v);
+}
+
+__device__ __forceinline__ f32x4_t scale_values(u32x2_t s) {
+  return f32x4_t{__uint_as_float(s[0] << 16), __uint_as_float(s[0] & 0xFFFF0000u), __uint_as_float(s[1] << 16),
+                 __uint_as_float(s[1] & 0xFFFF0000u)};
+}
 __device__ __forceinline__ f32x4_t scaled_add(f32x4_t sum, f32x4_t d, u32x2_t s) {
-  sum[0] = fmaf(d[0], __uint_as_float(s[0] << 16), sum[0]);
-  sum[1] = fmaf(d[1], __uint_as_float(s[0] & 0xFFFF0000u), sum[1]);
-  sum[2] = fmaf(d[2], __uint_as_float(s[1] << 16), sum[2]);
-  sum[3] = fmaf(d[3], __uint_as_float(s[1] & 0xFFFF0000u), sum[3]);
+  const f32x4_t v = scale_values(s);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum[i] = fmaf(d[i], v[i], sum[i]);
   return sum;
 }
 
@@ -226,6 +243,27 @@ __device__ __forceinline__ void few_store(const FewArgs &a, int n, int row, floa
   static_cast<T *>(a.out)[at] = from_f32<T>(sum);
 }
 
+// four neighbouring rows of it
+template <typename T>
+__device__ __forceinline__ void few_store4(const FewArgs &a, int n, int row, f32x4_t sum) {
+  const int64_t at = static_cast<int64_t>(n) * a.rows + row;
+  f32x4_t skip = kZero4;
+  if (a.residual) {
+    if constexpr (sizeof(T) == 4) {
+      skip = *reinterpret_cast<const f32x4_t *>(static_cast<const float *>(a.residual) + at);
+    } else {
+      const u32x2_t v = *reinterpret_cast<const u32x2_t *>(static_cast<const bf16_t *>(a.residual) + at);
+      skip = f32x4_t{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xFFFF0000u), __uint_as_float(v[1] << 16),
+                     __uint_as_float(v[1] & 0xFFFF0000u)};
+    }
+  }
+  const float scale = a.row_scale ? a.row_scale[n] : 1.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum[i] = sum[i] * scale + skip[i];
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4_t *>(static_cast<float *>(a.out) + at) = sum;
+  else *reinterpret_cast<u32x2_t *>(static_cast<bf16_t *>(a.out) + at) = u32x2_t{pack_bf16x2(sum[0], sum[1]), pack_bf16x2(sum[2], sum[3])};
+}
+
 // ---------------------------------------------------------------- up to eight slots
 // One pass over the picked experts' rows, bound by how many of their bytes are under way: a workgroup of eight wavefronts per
 // eight output rows, so that 2048 rows are a workgroup for every CU; the wavefronts deal the columns among
@@ -236,9 +274,9 @@ __device__ __forceinline__ void few_store(const FewArgs &a, int n, int row, floa
 // Plain rows: the two parts are the halves of a 128-byte line (64 columns; 32 in fp32).  4 bits: neighbouring blocks.
 // SWIGLU: eight gate and eight up rows; blockIdx.y is a slot, its expert that of the first slot that names it.  Else with K
 // == 1 the same; with K > 1 a workgroup meets every expert in turn and adds a token's slots.
-template <typename T, int G, bool SWIGLU>
+template <typename T, int G, bool SWIGLU, int RT>
 __global__ __launch_bounds__(512) void few_slots_kernel(const FewArgs a) {
-  constexpr int RT = SWIGLU ? 2 : 1, WAVES = 8;
+  constexpr int WAVES = 8;
   __shared__ __attribute__((aligned(16))) float red[WAVES][RT][2][8][8];    // wavefront, tile, part, slot, row
   __shared__ float sq[WAVES][8];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -292,7 +330,7 @@ __global__ __launch_bounds__(512) void few_slots_kernel(const FewArgs a) {
 #pragma unroll
     for (int t = 0; t < RT; ++t) acc[t] = kZero4;
     if constexpr (G == 0) {
-      constexpr int UNITS = sizeof(T) == 2 ? 4 : 2;
+      constexpr int UNITS = (sizeof(T) == 2 ? 4 : 2) / (RT > 2 ? 2 : 1);
       const int units = (a.cols + 63) / 64;
       for (int u0 = wave; u0 < units; u0 += WAVES * UNITS) {
         Eight<T> w[UNITS][RT], v[UNITS];
@@ -322,7 +360,7 @@ __global__ __launch_bounds__(512) void few_slots_kernel(const FewArgs a) {
       const int units = (m.col_blocks + 1) / 2, tile = row0 / 16, r0 = row0 % 16;
       for (int u0 = wave; u0 < units; u0 += WAVES * UNITS) {
         u32x4_t w[UNITS][RT];
-        u32x2_t scale[UNITS][RT][GROUPS];
+        u32x2_t scale[UNITS][RT];
         Eight<T> v[UNITS][4];
 #pragma unroll
         for (int i = 0; i < UNITS; ++i) {
@@ -330,9 +368,9 @@ __global__ __launch_bounds__(512) void few_slots_kernel(const FewArgs a) {
           const int b_in = b < m.col_blocks ? b : 0, db_in = db < m.col_blocks ? db : 0;
 #pragma unroll
           for (int t = 0; t < RT; ++t) {
-            w[i][t] = m.words(tile, b_in, q, r0 + 8 * t + c);
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g) scale[i][t][g] = m.scale4(tile, db_in, g, r0 + 8 * t + d_row);
+            const int r = r0 + 8 * t;                           // r0 is 0 where there is a second tile
+            w[i][t] = m.words(tile + r / 16, b_in, q, r % 16 + c);
+            scale[i][t] = m.scale4(tile + r / 16, db_in, r % 16 + d_row);
           }
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -360,7 +398,7 @@ __global__ __launch_bounds__(512) void few_slots_kernel(const FewArgs a) {
                 codes.codes(b < m.col_blocks ? w[i][t][j] : 0u);
                 d = mma(codes, v[i][j], d);
               }
-              acc[t] = scaled_add(acc[t], d, scale[i][t][g]);
+              acc[t] = scaled_add(acc[t], d, quad_lane(scale[i][t], g));
             }
         }
       }
@@ -381,16 +419,15 @@ __global__ __launch_bounds__(512) void few_slots_kernel(const FewArgs a) {
     if (lane < 8) sq[wave][lane] = squares;
   }
   __syncthreads();
-  if (tid >= 64) return;
-  // thread (slot, row): the wavefronts' sums in wavefront order
-  const int slot = tid >> 3, r = tid & 7;
-  float v[RT];
+  // wavefront i: tile i (a gate and an up tile with SWIGLU); thread (slot, row): the wavefronts' sums in wavefront order
+  if (wave >= RT / (SWIGLU ? 2 : 1)) return;
+  const int slot = lane >> 3, r = lane & 7;
+  const auto sum_of = [&](int t) __attribute__((always_inline)) {
+    float v = 0.0f;
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    v[t] = 0.0f;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) v[t] += red[w][t][0][slot][r] + red[w][t][1][slot][r];
-  }
+    for (int w = 0; w < WAVES; ++w) v += red[w][t][0][slot][r] + red[w][t][1][slot][r];
+    return v;
+  };
   int slot_expert = -1;
 #pragma unroll
   for (int i = 0; i < kFewSlots; ++i) slot_expert = i == slot ? expert[i] : slot_expert;
@@ -403,52 +440,53 @@ __global__ __launch_bounds__(512) void few_slots_kernel(const FewArgs a) {
       for (int w = 0; w < WAVES; ++w) sum += sq[w][slot];
       rstd = 1.0f / sqrtf(sum / a.cols + a.eps);
     }
-    static_cast<T *>(a.out)[static_cast<int64_t>(slot) * (a.rows / 2) + row0 / 2 + r] = from_f32<T>(silu_f32(v[0] * rstd) * (v[1] * rstd));
+    static_cast<T *>(a.out)[static_cast<int64_t>(slot) * (a.rows / 2) + row0 / 2 + 8 * wave + r] =
+        from_f32<T>(silu_f32(sum_of(2 * wave) * rstd) * (sum_of(2 * wave + 1) * rstd));
   } else {
-    float sum = v[0];
-    int n = slot;
+    float sum = sum_of(wave);
+    const int row = row0 + 8 * wave + r;
     if (a.K == 1) {
       if (slot >= S || (mine >= 0 ? slot_expert != mine : slot != y)) return;
       sum = mine >= 0 ? (a.gate ? a.gate[slot] * sum : sum) : 0.0f;
     } else {
-      float weighted = slot_expert >= 0 ? (a.gate ? a.gate[slot] * sum : sum) : 0.0f;
+      const float weighted = slot_expert >= 0 ? (a.gate ? a.gate[slot] * sum : sum) : 0.0f;
       sum = 0.0f;
       for (int k = 0; k < a.K; ++k) {
         const int src = (slot * a.K + k) * 8 + r;
         sum += __shfl(weighted, src < 64 ? src : r);
       }
-      if (n >= a.N) return;
+      if (slot >= a.N) return;
     }
-    few_store<T>(a, n, row0 + r, sum);
+    few_store<T>(a, slot, row, sum);
   }
 }
 
 // ---------------------------------------------------------------- more slots
-// A workgroup owns RT row tiles of 16 for up to 16 TT slots of one expert; its wavefronts deal the blocks of 128
-// columns among themselves, and their sums meet in LDS.  Nothing has been sorted for it: every workgroup counts the slots of
-// each expert and finds the blockIdx.y-th piece (an expert and up to 16 TT of its slots) by itself.
-template <typename T, int G, bool SWIGLU, int RT, int TT>
-__global__ __launch_bounds__(256) void many_slots_kernel(const FewArgs a) {
-  constexpr int WAVES = 4, ROWS = 16 * RT, COLS = 16 * TT;
-  __shared__ __attribute__((aligned(16))) float red[WAVES][COLS][ROWS + 4];
-  __shared__ float sq[WAVES][COLS];
-  __shared__ int count[kMaxExperts];
-  __shared__ signed char slot_expert[ROM_FEW_TOKENS * 8];
-  __shared__ int slots[COLS];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+// Nothing has been sorted for these kernels: every workgroup counts the slots of each expert and finds the blockIdx.y-th
+// piece, an expert and up to COLS of its slots, by itself.
+template <int COLS>
+struct Pieces {
+  int count[kMaxExperts];
+  int nobody;                  // slots that name no expert
+  signed char slot_expert[ROM_FEW_TOKENS * 8];
+  int slots[COLS];
+};
+template <typename T, bool SWIGLU, int COLS, int ROWS>
+__device__ __forceinline__ bool find_piece(const FewArgs &a, int row0, Pieces<COLS> &sh, int &e, int &n_cols) {
+  const int tid = threadIdx.x, lane = tid & 63, n_threads = blockDim.x;
   const int S = a.N * a.K;
-  const int row0 = blockIdx.x * ROWS;
-  if (tid < kMaxExperts) count[tid] = 0;
+  if (tid < kMaxExperts) sh.count[tid] = 0;
+  if (tid == 0) sh.nobody = 0;
   __syncthreads();
-  for (int s = tid; s < S; s += 256) {
-    int e = a.expert_idx ? a.expert_idx[s] : 0;
-    e = e >= 0 && e < a.n_mats ? e : -1;
-    slot_expert[s] = static_cast<signed char>(e);
-    if (e >= 0) atomicAdd(&count[e], 1);
+  for (int s = tid; s < S; s += n_threads) {
+    int v = a.expert_idx ? a.expert_idx[s] : 0;
+    v = v >= 0 && v < a.n_mats ? v : -1;
+    sh.slot_expert[s] = static_cast<signed char>(v);
+    atomicAdd(v >= 0 ? &sh.count[v] : &sh.nobody, 1);
   }
   __syncthreads();
-  // lane = expert: its pieces, and how many lie before them
-  const int mine = count[lane], pieces = (mine + COLS - 1) / COLS;
+  // lane = expert: its pieces, and how many there are up to it
+  const int mine = sh.count[lane], pieces = (mine + COLS - 1) / COLS;
   int upto = pieces;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
@@ -457,28 +495,45 @@ __global__ __launch_bounds__(256) void many_slots_kernel(const FewArgs a) {
   }
   if constexpr (!SWIGLU) {
     // slots that name no expert get the residual alone
-    if (a.K == 1 && blockIdx.y == 0) {
+    if (a.K == 1 && blockIdx.y == 0 && sh.nobody > 0) {
       for (int s = 0; s < S; ++s)
-        if (slot_expert[s] < 0)
-          for (int r = tid; r < ROWS && row0 + r < a.rows; r += 256) few_store<T>(a, s, row0 + r, 0.0f);
+        if (sh.slot_expert[s] < 0)
+          for (int r = tid; r < ROWS && row0 + r < a.rows; r += n_threads) few_store<T>(a, s, row0 + r, 0.0f);
     }
   }
   const unsigned long long past = __ballot(upto > static_cast<int>(blockIdx.y));
-  if (past == 0) return;
-  const int e = __builtin_ctzll(past);
+  if (past == 0) return false;
+  e = __builtin_ctzll(past);
   const int from = (static_cast<int>(blockIdx.y) - (__shfl(upto, e) - __shfl(pieces, e))) * COLS;
-  const int left = __shfl(mine, e) - from, n_cols = left < COLS ? left : COLS;
-  if (wave == 0) {
+  const int left = __shfl(mine, e) - from;
+  n_cols = __builtin_amdgcn_readfirstlane(left < COLS ? left : COLS);
+  if (tid < 64) {
     int seen = 0;
     for (int s0 = 0; s0 < S && seen < from + n_cols; s0 += 64) {
-      const bool in = s0 + lane < S && slot_expert[s0 + lane] == e;
+      const bool in = s0 + lane < S && sh.slot_expert[s0 + lane] == e;
       const unsigned long long b = __ballot(in);
       const int at = seen + __popcll(b & ((1ull << lane) - 1)) - from;
-      if (in && at >= 0 && at < n_cols) slots[at] = s0 + lane;
+      if (in && at >= 0 && at < n_cols) sh.slots[at] = s0 + lane;
       seen += __popcll(b);
     }
   }
   __syncthreads();
+  return true;
+}
+
+// Short calls: a workgroup owns RT row tiles of 16 for up to 16 TT slots of one expert; its wavefronts deal the blocks of 128
+// columns among themselves, and their sums meet in LDS.
+template <typename T, int G, bool SWIGLU, int RT, int TT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, 4))) void many_slots_kernel(const FewArgs a) {
+  constexpr int ROWS = 16 * RT, COLS = 16 * TT;
+  __shared__ __attribute__((aligned(16))) float red[WAVES][COLS][ROWS + 4];
+  __shared__ float sq[WAVES][COLS];
+  __shared__ Pieces<COLS> sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int row0 = blockIdx.x * ROWS;
+  int e, n_cols;
+  if (!find_piece<T, SWIGLU, COLS, ROWS>(a, row0, sh, e, n_cols)) return;
+  const int *slots = sh.slots;
 
   const int c = lane & 15, q = lane >> 4;
   const Matrix<T, G> m(a, e);
@@ -530,13 +585,12 @@ __global__ __launch_bounds__(256) void many_slots_kernel(const FewArgs a) {
     } else {
       constexpr int GROUPS = 128 / G;
       u32x4_t w[RT];
-      u32x2_t scale[RT][GROUPS];
+      u32x2_t scale[RT];
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
         const int tile = row0 + 16 * i < a.rows ? row0 / 16 + i : 0;
         w[i] = m.words(tile, b, q, c);
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) scale[i][g] = m.scale4(tile, b, g, 4 * q);
+        scale[i] = m.scale4(tile, b, 4 * q);
       }
 #pragma unroll
       for (int t = 0; t < TT; ++t)
@@ -557,7 +611,7 @@ __global__ __launch_bounds__(256) void many_slots_kernel(const FewArgs a) {
             for (int t = 0; t < TT; ++t) d[t] = mma(codes, v[t][j], d[t]);
           }
 #pragma unroll
-          for (int t = 0; t < TT; ++t) acc[i][t] = scaled_add(acc[i][t], d[t], scale[i][g]);
+          for (int t = 0; t < TT; ++t) acc[i][t] = scaled_add(acc[i][t], d[t], quad_lane(scale[i], g));
         }
     }
     if constexpr (SWIGLU) {
@@ -585,7 +639,7 @@ __global__ __launch_bounds__(256) void many_slots_kernel(const FewArgs a) {
     return v;
   };
   if constexpr (SWIGLU) {
-    for (int i = tid; i < n_cols * (ROWS / 2); i += 256) {
+    for (int i = tid; i < n_cols * (ROWS / 2); i += WAVES * 64) {
       const int col = i / (ROWS / 2), f = i % (ROWS / 2), r = f / 8 * 16 + f % 8;
       if (row0 + r >= a.rows) continue;
       float rstd = 1.0f;
@@ -599,13 +653,184 @@ __global__ __launch_bounds__(256) void many_slots_kernel(const FewArgs a) {
           from_f32<T>(silu_f32(total(col, r) * rstd) * (total(col, r + 8) * rstd));
     }
   } else {
-    for (int i = tid; i < n_cols * ROWS; i += 256) {
-      const int col = i / ROWS, r = i % ROWS, slot = slots[col];
+    for (int i = tid; i < n_cols * (ROWS / 4); i += WAVES * 64) {
+      const int col = i / (ROWS / 4), r = i % (ROWS / 4) * 4, slot = slots[col];
       if (row0 + r >= a.rows) continue;
-      float v = total(col, r);
+      f32x4_t v = kZero4;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) v += *reinterpret_cast<const f32x4_t *>(&red[w][col][r]);
       if (a.gate) v *= a.gate[slot];
-      if (a.K == 1) few_store<T>(a, slot, row0 + r, v);
-      else a.partial[static_cast<int64_t>(slot) * a.rows + row0 + r] = v;
+      if (a.K == 1) few_store4<T>(a, slot, row0 + r, v);
+      else *reinterpret_cast<f32x4_t *>(a.partial + static_cast<int64_t>(slot) * a.rows + row0 + r) = v;
+    }
+  }
+}
+
+// A load at a uniform address plus a lane's 32-bit offset; held here, so that no 64-bit address per lane is kept instead.
+template <typename V>
+__device__ __forceinline__ V load_at(const void *base, unsigned int offset) {
+  asm("" : "+s"(base));
+  return *reinterpret_cast<const V *>(static_cast<const char *>(base) + offset);
+}
+
+// Many slots an expert: reading their rows costs each CU more than the weights do, so that they are fetched once for
+// 128 RT rows.  A wavefront owns RT row tiles of 16 and all columns; a block of 128 columns of the piece's rows is in LDS for
+// the eight of them (pitch 272 bytes: the reads of 16 rows touch every bank once), the next block's rows and weights are on
+// their way in registers, one barrier a block.  No sum crosses wavefronts.
+template <int G, bool SWIGLU, int RT, int TT, int DEPTH, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, 4))) void shared_slots_kernel(const FewArgs a) {
+  constexpr int COLS = 16 * TT, ROWS = 16 * RT * WAVES, PITCH = 136, GROUPS = G ? 128 / (G ? G : 1) : 1;
+  constexpr int XS = 4 * WAVES, XT = (COLS + XS - 1) / XS;      // slots that are fetched together, that a thread fetches
+  __shared__ Pieces<COLS> sh;
+  __shared__ __attribute__((aligned(16))) bf16_t xs[2][XS * XT * PITCH];
+  __shared__ float rstd_of[XS * XT];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int row_wg = blockIdx.x * ROWS;
+  int e, n_cols;
+  if (!find_piece<bf16_t, SWIGLU, COLS, ROWS>(a, row_wg, sh, e, n_cols)) return;
+  const int used = (n_cols + 15) / 16;                          // column tiles
+  const int c = lane & 15, q = lane >> 4;
+  const int row0 = row_wg + wave * (16 * RT);
+  const Matrix<bf16_t, G> m(a, e);
+  const int nb = m.col_blocks;
+
+  // thread: columns 8 ch .. of a block, slots tid / 16 + 32 t
+  const int ch = tid & 15;
+  unsigned int x_at[XT];
+  float squares[XT];
+#pragma unroll
+  for (int t = 0; t < XT; ++t) {
+    const int col = tid / 16 + XS * t, slot = sh.slots[col < n_cols ? col : 0];
+    x_at[t] = (static_cast<unsigned int>(a.x_by_slot ? slot : slot / a.K) * a.cols + 8 * ch) * 2;      // below 2^32, see shared_takes
+    squares[t] = 0.0f;
+  }
+  f32x4_t acc[RT][TT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int t = 0; t < TT; ++t) acc[i][t] = kZero4;
+
+  // DEPTH blocks under way, each in registers of its own; blocks past the last are the last again, times zero
+  Eight<bf16_t> xr[DEPTH][XT];
+  u32x4_t w[DEPTH][RT][G ? 1 : 4];
+  u32x2_t scale[DEPTH][RT];
+  const unsigned int code_at = lane * 16, scale_at = ((lane & (GROUPS - 1)) * 16 + 4 * q) * 2;
+  const unsigned int plain_at = static_cast<unsigned int>(c) * a.cols * 2;
+  const auto fetch = [&](int u, int block) __attribute__((always_inline)) {
+    const int b = block < nb ? block : nb - 1;
+    const bool whole = 128 * b + 128 <= a.cols;                 // else: what lies past the row's end is read from its start
+    const unsigned int back = whole || 128 * b + 8 * ch < a.cols ? 0 : 16 * ch;
+#pragma unroll
+    for (int t = 0; t < XT; ++t) xr[u][t].v = load_at<u32x4_t>(static_cast<const bf16_t *>(a.x) + 128 * b, x_at[t] - back);
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      const int tile = row0 + 16 * i < a.rows ? row0 / 16 + i : 0;
+      if constexpr (G != 0) {
+        w[u][i][0] = load_at<u32x4_t>(m.codes + (static_cast<int64_t>(tile) * nb + b) * 1024, code_at);
+        scale[u][i] = load_at<u32x2_t>(m.scales + (static_cast<int64_t>(tile) * nb + b) * (GROUPS * 16), scale_at);
+      } else {
+        const unsigned int row_back = tile * 16 + c < a.rows ? 0 : 16 * a.cols;      // rows come in eights: the last tile may be half one
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const unsigned int col = whole || 128 * b + 32 * j + 8 * q < a.cols ? 64 * j + 16 * q : 0;
+          w[u][i][j] = load_at<u32x4_t>(m.plain + static_cast<int64_t>(tile) * 16 * a.cols + 128 * b, plain_at - row_back + col);
+        }
+      }
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < DEPTH; ++u) {
+    fetch(u, u);
+    __builtin_amdgcn_sched_barrier(0);                          // in the order of their use: waits count from the youngest
+  }
+  for (int b0 = 0; b0 < nb; b0 += DEPTH) {
+#pragma unroll
+    for (int u = 0; u < DEPTH; ++u) {
+      const int b = b0 + u;
+      const bool whole = 128 * b + 128 <= a.cols;
+      bf16_t *xb = xs[u & 1];
+#pragma unroll
+      for (int t = 0; t < XT; ++t) {
+        if (!whole) xr[u][t].zero_unless(128 * b + 8 * ch < a.cols);
+        if constexpr (SWIGLU) squares[t] = square_sum(xr[u][t], squares[t]);
+        *reinterpret_cast<u32x4_t *>(xb + (tid / 16 + XS * t) * PITCH + 8 * ch) = xr[u][t].v;
+      }
+      Eight<bf16_t> wf[RT][4];
+      f32x4_t sf[RT][GROUPS];
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        if constexpr (G != 0) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) wf[i][j].codes(w[u][i][0][j]);
+#pragma unroll
+          for (int g = 0; g < GROUPS; ++g) sf[i][g] = scale_values(quad_lane(scale[u][i], g));
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            wf[i][j].v = w[u][i][j];
+            if (!whole) wf[i][j].zero_unless(128 * b + 32 * j + 8 * q < a.cols);
+          }
+        }
+      }
+      fetch(u, b + DEPTH);                                      // in any case: a branch here would wait for what it requests
+      __syncthreads();
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        if (t >= used) continue;
+        Eight<bf16_t> v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j].load(xb + (16 * t + c) * PITCH + 32 * j + 8 * q);
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+          for (int g = 0; g < GROUPS; ++g) {
+            f32x4_t d = G ? kZero4 : acc[i][t];
+#pragma unroll
+            for (int j = g * (4 / GROUPS); j < (g + 1) * (4 / GROUPS); ++j) d = mma(wf[i][j], v[j], d);
+            if constexpr (G != 0) {
+#pragma unroll
+              for (int r = 0; r < 4; ++r) acc[i][t][r] = fmaf(d[r], sf[i][g][r], acc[i][t][r]);
+            } else {
+              acc[i][t] = d;
+            }
+          }
+      }
+    }
+  }
+  if constexpr (SWIGLU) {
+#pragma unroll
+    for (int t = 0; t < XT; ++t) {
+#pragma unroll
+      for (int d = 1; d < 16; d <<= 1) squares[t] += __shfl_xor(squares[t], d);
+      if (ch == 0) rstd_of[tid / 16 + XS * t] = a.norm ? 1.0f / sqrtf(squares[t] / a.cols + a.eps) : 1.0f;
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int t = 0; t < TT; ++t) {
+    const int col = 16 * t + c;
+    if (t >= used) continue;
+    const int slot = sh.slots[col < n_cols ? col : 0];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      const int row = row0 + 16 * i + 4 * q;
+      if constexpr (SWIGLU) {                                   // up feature of gate row r: row r + 8, held by lane + 32
+        f32x4_t up;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) up[r] = __shfl_xor(acc[i][t][r], 32);
+        if (q < 2 && col < n_cols && row < a.rows) {
+          const float rstd = rstd_of[col];
+          float h[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) h[r] = silu_f32(acc[i][t][r] * rstd) * (up[r] * rstd);
+          *reinterpret_cast<u32x2_t *>(static_cast<bf16_t *>(a.out) + static_cast<int64_t>(slot) * (a.rows / 2) + (row0 + 16 * i) / 2 + 4 * q) =
+              u32x2_t{pack_bf16x2(h[0], h[1]), pack_bf16x2(h[2], h[3])};
+        }
+      } else if (col < n_cols && row < a.rows) {
+        const f32x4_t v = acc[i][t] * (a.gate ? a.gate[slot] : 1.0f);
+        if (a.K == 1) few_store4<bf16_t>(a, slot, row, v);
+        else *reinterpret_cast<f32x4_t *>(a.partial + static_cast<int64_t>(slot) * a.rows + row) = v;
+      }
     }
   }
 }
@@ -613,15 +838,15 @@ __global__ __launch_bounds__(256) void many_slots_kernel(const FewArgs a) {
 // K > 1: a token's weighted slots, in slot order
 template <typename T>
 __global__ __launch_bounds__(256) void few_combine_kernel(const FewArgs a) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
   if (i >= static_cast<int64_t>(a.N) * a.rows) return;
   const int n = static_cast<int>(i / a.rows), row = static_cast<int>(i % a.rows);
-  float sum = 0.0f;
+  f32x4_t sum = kZero4;
   for (int k = 0; k < a.K; ++k) {
     const int slot = n * a.K + k, e = a.expert_idx[slot];
-    if (e >= 0 && e < a.n_mats) sum += a.partial[static_cast<int64_t>(slot) * a.rows + row];
+    if (e >= 0 && e < a.n_mats) sum += *reinterpret_cast<const f32x4_t *>(a.partial + static_cast<int64_t>(slot) * a.rows + row);
   }
-  few_store<T>(a, n, row, sum);
+  few_store4<T>(a, n, row, sum);
 }
 
 unsigned blocks_of(int64_t n, int per) { return static_cast<unsigned>(ceil_div(n, per)); }
@@ -647,36 +872,59 @@ hipError_t convert_group(bool pack, const void *w, int n_mats, int rows, int col
                        : convert<T, 128>(pack, w, n_mats, rows, cols, w_q4, s);
 }
 
-template <typename T, int G, bool SWIGLU, int RT, int TT>
-void launch_many(const FewArgs &a, hipStream_t s) {
+// shared_slots_kernel holds a lane's place in x in 32 bits
+bool shared_takes(const FewArgs &a) { return static_cast<int64_t>(a.x_by_slot ? a.N * a.K : a.N) * a.cols * 2 < (1ll << 32); }
+
+// pieces: at most one that is not full for every expert met
+unsigned most_pieces(const FewArgs &a, int cols) {
   const int S = a.N * a.K;
-  // pieces: at most one that is not full for every expert met
-  const int pieces = (S < a.n_mats ? S : a.n_mats) + S / (16 * TT);
-  hipLaunchKernelGGL((many_slots_kernel<T, G, SWIGLU, RT, TT>), dim3(blocks_of(a.rows, 16 * RT), pieces), dim3(256), 0, s, a);
+  return static_cast<unsigned>((S < a.n_mats ? S : a.n_mats) + S / cols);
 }
+
+template <typename T, int G, bool SWIGLU, int RT, int TT, int WAVES>
+void launch_many(const FewArgs &a, hipStream_t s) {
+  hipLaunchKernelGGL((many_slots_kernel<T, G, SWIGLU, RT, TT, WAVES>), dim3(blocks_of(a.rows, 16 * RT), most_pieces(a, 16 * TT)),
+                     dim3(WAVES * 64), 0, s, a);
+}
+template <int G, bool SWIGLU, int RT, int TT, int DEPTH, int WAVES>
+void launch_shared(const FewArgs &a, hipStream_t s) {
+  hipLaunchKernelGGL((shared_slots_kernel<G, SWIGLU, RT, TT, DEPTH, WAVES>), dim3(blocks_of(a.rows, 16 * RT * WAVES), most_pieces(a, 16 * TT)),
+                     dim3(WAVES * 64), 0, s, a);
+}
+
+constexpr int kFewWide = 256;       // row blocks of a double width from which few_slots_kernel takes them (4 bits)
+constexpr int kManyAvg = 8;         // slots per expert met up to which the weights are most of what a workgroup reads
 
 template <typename T, int G, bool SWIGLU>
 hipError_t launch_form(const FewArgs &a, hipStream_t s) {
   const int S = a.N * a.K;
   if (S <= kFewSlots) {
-    hipLaunchKernelGGL((few_slots_kernel<T, G, SWIGLU>), dim3(a.rows / (SWIGLU ? 16 : 8), SWIGLU || a.K == 1 ? S : 1), dim3(512), 0, s, a);
+    const dim3 block(512);
+    const int y = SWIGLU || a.K == 1 ? S : 1;
+    constexpr int TILES = SWIGLU ? 2 : 1;                       // of eight rows
+    if (G != 0 && a.rows % (16 * TILES) == 0 && a.rows / (16 * TILES) >= kFewWide)
+      hipLaunchKernelGGL((few_slots_kernel<T, G, SWIGLU, 2 * TILES>), dim3(a.rows / (16 * TILES), y), block, 0, s, a);
+    else
+      hipLaunchKernelGGL((few_slots_kernel<T, G, SWIGLU, TILES>), dim3(a.rows / (8 * TILES), y), block, 0, s, a);
     return hipGetLastError();
   }
+  const int met = S < a.n_mats ? S : a.n_mats;                  // experts, at most
+  const bool dense = S > kManyAvg * met;
   if constexpr (sizeof(T) == 4) {
-    launch_many<T, G, SWIGLU, 1, 1>(a, s);
+    launch_many<T, G, SWIGLU, 1, 1, 8>(a, s);
+  } else if constexpr (G == 0) {
+    if (dense && shared_takes(a)) launch_shared<G, SWIGLU, 1, 4, 2, 4>(a, s);
+    else if (!SWIGLU && a.rows / 16 * met <= 2048) launch_many<T, G, SWIGLU, 1, 1, 8>(a, s);
+    else launch_many<T, G, SWIGLU, 2, 1, 4>(a, s);
+  } else if constexpr (SWIGLU) {
+    if (dense && shared_takes(a)) launch_shared<G, SWIGLU, 2, 2, 2, 4>(a, s);
+    else launch_many<T, G, SWIGLU, 4, 1, 4>(a, s);
   } else {
-    const int64_t met = S < a.n_mats ? S : a.n_mats;
-    const bool narrow = S <= 8 * met;
-    if (a.rows / 64 * met >= 512) {
-      if (narrow) launch_many<T, G, SWIGLU, 4, 1>(a, s);
-      else launch_many<T, G, SWIGLU, 4, 2>(a, s);
-    } else {
-      if (narrow) launch_many<T, G, SWIGLU, 2, 1>(a, s);
-      else launch_many<T, G, SWIGLU, 2, 2>(a, s);
-    }
+    if (dense) launch_many<T, G, SWIGLU, 4, 1, 4>(a, s);
+    else launch_many<T, G, SWIGLU, 2, 1, 4>(a, s);
   }
   if (!SWIGLU && a.K > 1)
-    hipLaunchKernelGGL(few_combine_kernel<T>, dim3(blocks_of(static_cast<int64_t>(a.N) * a.rows, 256)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(few_combine_kernel<T>, dim3(blocks_of(static_cast<int64_t>(a.N) * a.rows, 1024)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
