@@ -493,8 +493,8 @@ ROM_API int rom_q4_project(int dtype, const void *w_q4, int32_t n_mats, int32_t 
                            void *hip_stream);
 
 /* The FFN-MoE layer of rom_ffn_moe_forward for a few tokens: pre-norm, gate | up, SwiGLU, down, gate-weighted sum
- * and skip in two launches (three with top_k > 1 and more than 8 slots), straight from the routing
- * decision, without its grouping.
+ * and skip in two launches (three with top_k > 1 and several tokens), straight from the routing decision,
+ * without its grouping.
  *   w            q4_group 0: as rom_ffn_moe_forward takes them (w_gate_up in the packed row order).  q4_group
  *                32, 64 or 128: both packed by rom_q4_pack with that group (w_gate_up after
  *                rom_ffn_pack_gate_up: [E, 2*d_ff, d_model] and [E, d_model, d_ff])

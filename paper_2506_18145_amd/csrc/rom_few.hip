@@ -5,8 +5,6 @@
 namespace rom {
 namespace {
 
-constexpr int kFewSlots = 8;        // slots that one workgroup of few_slots_kernel meets together
-
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
@@ -264,57 +262,42 @@ __device__ __forceinline__ void few_store4(const FewArgs &a, int n, int row, f32
   else *reinterpret_cast<u32x2_t *>(static_cast<bf16_t *>(a.out) + at) = u32x2_t{pack_bf16x2(sum[0], sum[1]), pack_bf16x2(sum[2], sum[3])};
 }
 
-// ---------------------------------------------------------------- up to eight slots
+// ---------------------------------------------------------------- one token
 // One pass over the picked experts' rows, bound by how many of their bytes are under way: a workgroup of eight wavefronts per
-// eight output rows, so that 2048 rows are a workgroup for every CU; the wavefronts deal the columns among
-// themselves, nothing but registers between a request and its product, and their sums meet in LDS.  The 16 x 16 matrix
-// instruction holds eight rows twice, columns 8 .. 15 of both operands being another part of the inner dimension:
+// eight output rows, so that 2048 rows are a workgroup for every CU; the wavefronts deal the columns among themselves, nothing
+// but registers between a request and its product, and their sums meet in LDS.  The 16 x 16 matrix instruction holds eight
+// rows twice, columns 8 .. 15 of both operands being another part of the inner dimension:
 //   D[r][c] = first part,  D[8 + r][8 + c] = second part,  the other two quarters mean nothing.
-// A column is a slot, so that an expert that a token names twice is nothing special, and a slot never sees another's values.
-// Plain rows: the two parts are the halves of a 128-byte line (64 columns; 32 in fp32).  4 bits: neighbouring blocks.
-// SWIGLU: eight gate and eight up rows; blockIdx.y is a slot, its expert that of the first slot that names it.  Else with K
-// == 1 the same; with K > 1 a workgroup meets every expert in turn and adds a token's slots.
-template <typename T, int G, bool SWIGLU, int RT>
-__global__ __launch_bounds__(512) void few_slots_kernel(const FewArgs a) {
-  constexpr int WAVES = 8;
-  __shared__ __attribute__((aligned(16))) float red[WAVES][RT][2][8][8];    // wavefront, tile, part, slot, row
-  __shared__ float sq[WAVES][8];
+// A column is one of the token's up to eight slots, so that an expert that it names twice is nothing special.  Plain rows: the
+// two parts are the halves of a 128-byte line (64 columns).  4 bits: neighbouring blocks.
+// SWIGLU (one slot): eight gate and eight up rows.  Else the workgroup meets the token's experts in turn and adds its slots: no
+// launch for that.  d_model 2048, d_ff 4096: bf16 9.4 + 6.3 us (10.5 + 8.1 by many_slots_kernel), 4 bits down 4.8 (5.8).
+template <typename T, int G, bool SWIGLU>
+__global__ __launch_bounds__(512) void one_token_kernel(const FewArgs a) {
+  constexpr int WAVES = 8, SLOTS = 8, RT = SWIGLU ? 2 : 1;
+  __shared__ __attribute__((aligned(16))) float red[WAVES][RT][2][SLOTS][8];    // wavefront, tile, part, slot, row
+  __shared__ float sq[WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int S = a.N * a.K;
   const int row0 = blockIdx.x * (8 * RT);
-  int expert[kFewSlots];
+  int expert[SLOTS];
+  unsigned int first = 0;                                       // bit s: slot s is the first that names its expert
 #pragma unroll
-  for (int i = 0; i < kFewSlots; ++i) {
-    const int e = i < S ? (a.expert_idx ? a.expert_idx[i] : 0) : -1;
+  for (int i = 0; i < SLOTS; ++i) {
+    const int e = i < a.K ? (a.expert_idx ? a.expert_idx[i] : 0) : -1;
     expert[i] = e >= 0 && e < a.n_mats ? e : -1;
-  }
-  // bit s: slot s is the first that names its expert
-  unsigned int first = 0;
-#pragma unroll
-  for (int i = 0; i < kFewSlots; ++i) {
     bool seen = expert[i] < 0;
 #pragma unroll
     for (int j = 0; j < i; ++j) seen = seen || expert[j] == expert[i];
     first |= seen ? 0u : 1u << i;
   }
-  const bool by_slot = SWIGLU || a.K == 1;
-  const int y = blockIdx.y;
-  int mine = -1;                                                // by_slot: this workgroup's expert
-#pragma unroll
-  for (int i = 0; i < kFewSlots; ++i) mine = i == y ? expert[i] : mine;
-  if (by_slot) {
-    if (mine >= 0 && !((first >> y) & 1u)) return;              // another workgroup's
-    if (SWIGLU && mine < 0) return;
-    first &= 1u << y;
-  }
+  if (SWIGLU && first == 0) return;
 
   const int c = lane & 7, part = (lane >> 3) & 1, q = lane >> 4;      // operands: row or slot c, part, columns 8 q .. of a step
   const int d_part = q >> 1, d_row = 4 * (q & 1);                     // result: rows d_row .. + 3 of part d_part, column lane & 15
   int my_expert = -1;                                           // of slot c
 #pragma unroll
-  for (int i = 0; i < kFewSlots; ++i) my_expert = i == c ? expert[i] : my_expert;
-  const int x_slot = c < S ? c : S - 1;
-  const T *x = static_cast<const T *>(a.x) + static_cast<int64_t>(a.x_by_slot ? x_slot : x_slot / a.K) * a.cols;
+  for (int i = 0; i < SLOTS; ++i) my_expert = i == c ? expert[i] : my_expert;
+  const T *x = static_cast<const T *>(a.x) + static_cast<int64_t>(a.x_by_slot ? (c < a.K ? c : a.K - 1) : 0) * a.cols;
 
   f32x4_t total[RT];
 #pragma unroll
@@ -324,13 +307,13 @@ __global__ __launch_bounds__(512) void few_slots_kernel(const FewArgs a) {
     const int s = __builtin_ctz(left);
     int e = -1;
 #pragma unroll
-    for (int i = 0; i < kFewSlots; ++i) e = i == s ? expert[i] : e;
+    for (int i = 0; i < SLOTS; ++i) e = i == s ? expert[i] : e;
     const Matrix<T, G> m(a, e);
     f32x4_t acc[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) acc[t] = kZero4;
     if constexpr (G == 0) {
-      constexpr int UNITS = (sizeof(T) == 2 ? 4 : 2) / (RT > 2 ? 2 : 1);
+      constexpr int UNITS = sizeof(T) == 2 ? 4 : 2;
       const int units = (a.cols + 63) / 64;
       for (int u0 = wave; u0 < units; u0 += WAVES * UNITS) {
         Eight<T> w[UNITS][RT], v[UNITS];
@@ -356,22 +339,18 @@ __global__ __launch_bounds__(512) void few_slots_kernel(const FewArgs a) {
         }
       }
     } else {
+      static_assert(!SWIGLU, "4 bits: many_slots_kernel");
       constexpr int UNITS = sizeof(T) == 2 ? 2 : 1, GROUPS = 128 / G;
       const int units = (m.col_blocks + 1) / 2, tile = row0 / 16, r0 = row0 % 16;
       for (int u0 = wave; u0 < units; u0 += WAVES * UNITS) {
-        u32x4_t w[UNITS][RT];
-        u32x2_t scale[UNITS][RT];
+        u32x4_t w[UNITS];
+        u32x2_t scale[UNITS];
         Eight<T> v[UNITS][4];
 #pragma unroll
         for (int i = 0; i < UNITS; ++i) {
           const int b = 2 * (u0 + i * WAVES) + part, db = 2 * (u0 + i * WAVES) + d_part;
-          const int b_in = b < m.col_blocks ? b : 0, db_in = db < m.col_blocks ? db : 0;
-#pragma unroll
-          for (int t = 0; t < RT; ++t) {
-            const int r = r0 + 8 * t;                           // r0 is 0 where there is a second tile
-            w[i][t] = m.words(tile + r / 16, b_in, q, r % 16 + c);
-            scale[i][t] = m.scale4(tile + r / 16, db_in, r % 16 + d_row);
-          }
+          w[i] = m.words(tile, b < m.col_blocks ? b : 0, q, r0 + c);
+          scale[i] = m.scale4(tile, db < m.col_blocks ? db : 0, r0 + d_row);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const int k = 128 * b + 32 * j + 8 * q;
@@ -383,23 +362,17 @@ __global__ __launch_bounds__(512) void few_slots_kernel(const FewArgs a) {
         for (int i = 0; i < UNITS; ++i) {
           const int b = 2 * (u0 + i * WAVES) + part;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            v[i][j].zero_unless(128 * b + 32 * j + 8 * q < a.cols);
-            if constexpr (SWIGLU) squares = square_sum(v[i][j], squares);
-          }
+          for (int g = 0; g < GROUPS; ++g) {
+            f32x4_t d = kZero4;
 #pragma unroll
-          for (int t = 0; t < RT; ++t)
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g) {
-              f32x4_t d = kZero4;
-#pragma unroll
-              for (int j = g * (4 / GROUPS); j < (g + 1) * (4 / GROUPS); ++j) {
-                Eight<T> codes;
-                codes.codes(b < m.col_blocks ? w[i][t][j] : 0u);
-                d = mma(codes, v[i][j], d);
-              }
-              acc[t] = scaled_add(acc[t], d, quad_lane(scale[i][t], g));
+            for (int j = g * (4 / GROUPS); j < (g + 1) * (4 / GROUPS); ++j) {
+              Eight<T> codes;
+              codes.codes(b < m.col_blocks ? w[i][j] : 0u);
+              v[i][j].zero_unless(128 * b + 32 * j + 8 * q < a.cols);
+              d = mma(codes, v[i][j], d);
             }
+            acc[0] = scaled_add(acc[0], d, quad_lane(scale[i], g));
+          }
         }
       }
     }
@@ -416,52 +389,41 @@ __global__ __launch_bounds__(512) void few_slots_kernel(const FewArgs a) {
     squares += __shfl_xor(squares, 8);
     squares += __shfl_xor(squares, 16);
     squares += __shfl_xor(squares, 32);
-    if (lane < 8) sq[wave][lane] = squares;
+    if (lane == 0) sq[wave] = squares;
   }
   __syncthreads();
-  // wavefront i: tile i (a gate and an up tile with SWIGLU); thread (slot, row): the wavefronts' sums in wavefront order
-  if (wave >= RT / (SWIGLU ? 2 : 1)) return;
+  if (wave != 0) return;
+  // lane (slot, row): the wavefronts' sums in wavefront order
   const int slot = lane >> 3, r = lane & 7;
-  const auto sum_of = [&](int t) __attribute__((always_inline)) {
-    float v = 0.0f;
+  float v[RT];
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) v += red[w][t][0][slot][r] + red[w][t][1][slot][r];
-    return v;
-  };
-  int slot_expert = -1;
+  for (int t = 0; t < RT; ++t) {
+    v[t] = 0.0f;
 #pragma unroll
-  for (int i = 0; i < kFewSlots; ++i) slot_expert = i == slot ? expert[i] : slot_expert;
+    for (int w = 0; w < WAVES; ++w) v[t] += red[w][t][0][slot][r] + red[w][t][1][slot][r];
+  }
   if constexpr (SWIGLU) {
-    if (slot >= S || slot_expert != mine) return;
+    if (slot > 0) return;
     float rstd = 1.0f;
     if (a.norm) {
       float sum = 0.0f;
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) sum += sq[w][slot];
+      for (int w = 0; w < WAVES; ++w) sum += sq[w];
       rstd = 1.0f / sqrtf(sum / a.cols + a.eps);
     }
-    static_cast<T *>(a.out)[static_cast<int64_t>(slot) * (a.rows / 2) + row0 / 2 + 8 * wave + r] =
-        from_f32<T>(silu_f32(sum_of(2 * wave) * rstd) * (sum_of(2 * wave + 1) * rstd));
+    static_cast<T *>(a.out)[row0 / 2 + r] = from_f32<T>(silu_f32(v[0] * rstd) * (v[1] * rstd));
   } else {
-    float sum = sum_of(wave);
-    const int row = row0 + 8 * wave + r;
-    if (a.K == 1) {
-      if (slot >= S || (mine >= 0 ? slot_expert != mine : slot != y)) return;
-      sum = mine >= 0 ? (a.gate ? a.gate[slot] * sum : sum) : 0.0f;
-    } else {
-      const float weighted = slot_expert >= 0 ? (a.gate ? a.gate[slot] * sum : sum) : 0.0f;
-      sum = 0.0f;
-      for (int k = 0; k < a.K; ++k) {
-        const int src = (slot * a.K + k) * 8 + r;
-        sum += __shfl(weighted, src < 64 ? src : r);
-      }
-      if (slot >= a.N) return;
-    }
-    few_store<T>(a, slot, row, sum);
+    int slot_expert = -1;
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) slot_expert = i == slot ? expert[i] : slot_expert;
+    const float weighted = slot_expert >= 0 ? (a.gate ? a.gate[slot] * v[0] : v[0]) : 0.0f;      // slots past K name no expert
+    float sum = 0.0f;
+    for (int k = 0; k < a.K; ++k) sum += __shfl(weighted, k * 8 + r);
+    if (slot == 0) few_store<T>(a, 0, row0 + r, sum);
   }
 }
 
-// ---------------------------------------------------------------- more slots
+// ---------------------------------------------------------------- several tokens
 // Nothing has been sorted for these kernels: every workgroup counts the slots of each expert and finds the blockIdx.y-th
 // piece, an expert and up to COLS of its slots, by itself.
 template <int COLS>
@@ -835,7 +797,7 @@ __global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, 4
   }
 }
 
-// K > 1: a token's weighted slots, in slot order
+// K > 1: a token's weighted slots from their several workgroups, in slot order
 template <typename T>
 __global__ __launch_bounds__(256) void few_combine_kernel(const FewArgs a) {
   const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
@@ -892,35 +854,42 @@ void launch_shared(const FewArgs &a, hipStream_t s) {
                      dim3(WAVES * 64), 0, s, a);
 }
 
-constexpr int kFewWide = 256;       // row blocks of a double width from which few_slots_kernel takes them (4 bits)
-constexpr int kManyAvg = 8;         // slots per expert met up to which the weights are most of what a workgroup reads
+// Which kernel takes a call.  Times in us, kernels alone, d_model 2048, d_ff 4096, 8 experts, top-1 unless another size stands there.
+//  one token             one_token_kernel, but for gate | up in 4 bits (6.3 against 7.2) and 4-bit projections of 4096 rows and
+//                        more (8192 x 2048: 5.4 against 7.2), which have row tiles enough for the other kernel
+//  many slots an expert  shared_slots_kernel where the weights are no longer most of what comes into a CU.  Gate | up, 4 bits:
+//                        32 slots 29.5 against 39.8, 16 24.4 against 27.4, 8 21.5 against 18.8.  bf16: 32 slots 70 + 41 against
+//                        92 + 57, 4 67 + 38 against 55 + 29.  Not the 4-bit projection (32 slots 23.7 against 28.9).
+//  else                  many_slots_kernel: few row tiles in short calls (enough workgroups), more in long ones (less of x):
+//                        the 4-bit projection with 8 wavefronts up to 512 workgroups (4 tokens 6.5 against 8.1), with 4 beyond (64
+//                        tokens 12.5 against 13.6), of four row tiles from 8 slots an expert on (32: 23.7 against 31.5)
+constexpr int kOneTokenRows = 4096;
+constexpr int kManyAvg = 8;
 
 template <typename T, int G, bool SWIGLU>
 hipError_t launch_form(const FewArgs &a, hipStream_t s) {
   const int S = a.N * a.K;
-  if (S <= kFewSlots) {
-    const dim3 block(512);
-    const int y = SWIGLU || a.K == 1 ? S : 1;
-    constexpr int TILES = SWIGLU ? 2 : 1;                       // of eight rows
-    if (G != 0 && a.rows % (16 * TILES) == 0 && a.rows / (16 * TILES) >= kFewWide)
-      hipLaunchKernelGGL((few_slots_kernel<T, G, SWIGLU, 2 * TILES>), dim3(a.rows / (16 * TILES), y), block, 0, s, a);
-    else
-      hipLaunchKernelGGL((few_slots_kernel<T, G, SWIGLU, TILES>), dim3(a.rows / (8 * TILES), y), block, 0, s, a);
-    return hipGetLastError();
+  if constexpr (!SWIGLU || G == 0) {
+    if (SWIGLU ? S == 1 : a.N == 1 && (G == 0 || a.rows < kOneTokenRows)) {
+      hipLaunchKernelGGL((one_token_kernel<T, G, SWIGLU>), dim3(a.rows / (SWIGLU ? 16 : 8)), dim3(512), 0, s, a);
+      return hipGetLastError();
+    }
   }
-  const int met = S < a.n_mats ? S : a.n_mats;                  // experts, at most
+  const int64_t met = S < a.n_mats ? S : a.n_mats;              // experts, at most
   const bool dense = S > kManyAvg * met;
   if constexpr (sizeof(T) == 4) {
-    launch_many<T, G, SWIGLU, 1, 1, 8>(a, s);
+    launch_many<T, G, SWIGLU, 1, 1, 4>(a, s);
   } else if constexpr (G == 0) {
     if (dense && shared_takes(a)) launch_shared<G, SWIGLU, 1, 4, 2, 4>(a, s);
     else if (!SWIGLU && a.rows / 16 * met <= 2048) launch_many<T, G, SWIGLU, 1, 1, 8>(a, s);
     else launch_many<T, G, SWIGLU, 2, 1, 4>(a, s);
   } else if constexpr (SWIGLU) {
     if (dense && shared_takes(a)) launch_shared<G, SWIGLU, 2, 2, 2, 4>(a, s);
+    else if (a.rows / 64 * met < 512) launch_many<T, G, SWIGLU, 2, 1, 8>(a, s);
     else launch_many<T, G, SWIGLU, 4, 1, 4>(a, s);
   } else {
     if (dense) launch_many<T, G, SWIGLU, 4, 1, 4>(a, s);
+    else if (a.rows / 32 * met <= 512) launch_many<T, G, SWIGLU, 2, 1, 8>(a, s);
     else launch_many<T, G, SWIGLU, 2, 1, 4>(a, s);
   }
   if (!SWIGLU && a.K > 1)
@@ -951,8 +920,8 @@ hipError_t launch_q4_unpack(int dtype, const void *w_q4, int n_mats, int rows, i
                                  : convert_group<float>(false, w, n_mats, rows, cols, group, q, s);
 }
 
-// a slot's products where a token has several slots and the call is too large for one workgroup to meet them all
-size_t few_partial_bytes(int64_t rows, int K, int64_t N) { return K > 1 && N * K > kFewSlots ? static_cast<size_t>(N * K * rows) * 4 : 0; }
+// every slot's products, where a token's slots come from several workgroups (one token of a wide 4-bit projection among them)
+size_t few_partial_bytes(int64_t rows, int K, int64_t N) { return K > 1 ? static_cast<size_t>(N * K * rows) * 4 : 0; }
 
 hipError_t launch_few(const FewArgs &a, hipStream_t s) {
   if (a.dtype == ROM_DTYPE_BF16) return a.swiglu ? launch_group<bf16_t, true>(a, s) : launch_group<bf16_t, false>(a, s);
