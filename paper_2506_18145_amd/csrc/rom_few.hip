@@ -75,6 +75,44 @@ __device__ __forceinline__ unsigned int q4_code(float w, float s) {
   return s > 0.0f && m > 0 ? m | (w < 0.0f ? 8u : 0u) : 0u;
 }
 
+// The same of eight bf16 weights at once: |w| / s to half a unit in the last place (a product with 1 / s and one correction, which
+// leaves a representable quotient as it is), rounded by the conversion to nearest even, 6 above it.  The quotient of two bf16 numbers
+// is a midpoint or differs from it by 2^-17 of it, so that the fp32 one lies on the same side; fp32 weights can be closer.  s at
+// least 1e-30.
+__device__ __forceinline__ unsigned int q4_word(const Eight<bf16_t> &w, float s, float inv) {
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float x = w.at(i), ratio = x * inv;
+    v[i] = fmaf(fmaf(-ratio, s, x), inv, ratio);
+  }
+  unsigned int word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v[0], v[1], 1.0f, 0);
+  word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[2], v[3], 1.0f, 1);
+  word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[4], v[5], 1.0f, 2);
+  word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[6], v[7], 1.0f, 3);
+  const unsigned int size = word & 0x77777777u, some = (size | size >> 1 | size >> 2) & 0x11111111u;
+  return size | (word & some << 3);                             // no negative zeros
+}
+
+// the largest size of eight values as an fp32 number, at least infinity where one of them is not finite
+__device__ __forceinline__ float largest(const Eight<bf16_t> &v) {
+  typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+  u16x2_t top = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2_t, v.v[i] & 0x7FFF7FFFu));
+  const unsigned short m = top[0] > top[1] ? top[0] : top[1];
+  return bf16_to_f32(m < 0x7F80 ? m : 0x7F80);
+}
+__device__ __forceinline__ float largest(const Eight<float> &v) {
+  float top = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float a = fabsf(v.at(i));
+    top = fmaxf(top, a < __builtin_inff() ? a : __builtin_inff());      // a NaN does not pass fmaxf
+  }
+  return top;
+}
+
 struct Q4Block {
   int64_t block, mat, row, scale;      // scale: index of group 0 of the block, row included
   int col, r, q;                       // first column of the block
@@ -114,25 +152,24 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const T *__restrict__ w, i
   u32x4_t out;
 #pragma unroll
   for (int g = 0; g < 128 / G; ++g) {
-    // the largest size over the group, infinity where something in it is not finite (a NaN does not pass fmaxf)
     float top = 0.0f;
 #pragma unroll
-    for (int j = g * (G / 32); j < (g + 1) * (G / 32); ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float a = fabsf(v[j].at(i));
-        top = fmaxf(top, a < __builtin_inff() ? a : __builtin_inff());
-      }
+    for (int j = g * (G / 32); j < (g + 1) * (G / 32); ++j) top = fmaxf(top, largest(v[j]));
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
     const bf16_t bits = top < __builtin_inff() ? f32_to_bf16(top / 6.0f) : static_cast<bf16_t>(0x7FC0);
-    const float s = bf16_to_f32(bits);
+    const float s = bf16_to_f32(bits), inv = 1.0f / s;
 #pragma unroll
     for (int j = g * (G / 32); j < (g + 1) * (G / 32); ++j) {
-      unsigned int word = 0;
+      out[j] = 0;
+      if constexpr (sizeof(T) == 2) {
+        if (s >= 1e-30f) {
+          out[j] = q4_word(v[j], s, inv);
+          continue;
+        }
+      }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) word |= q4_code(v[j].at(i), s) << (4 * i);
-      out[j] = word;
+      for (int i = 0; i < 8; ++i) out[j] |= q4_code(v[j].at(i), s) << (4 * i);
     }
     if (b.q == 0) scales[b.scale + g * 16] = bits;
   }
