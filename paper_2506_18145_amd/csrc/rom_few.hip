@@ -871,13 +871,15 @@ hipError_t convert_group(bool pack, const void *w, int n_mats, int rows, int col
                        : convert<T, 128>(pack, w, n_mats, rows, cols, w_q4, s);
 }
 
-// shared_slots_kernel holds a lane's place in x in 32 bits
-bool shared_takes(const FewArgs &a) { return static_cast<int64_t>(a.x_by_slot ? a.N * a.K : a.N) * a.cols * 2 < (1ll << 32); }
-
 // pieces: at most one that is not full for every expert met
 unsigned most_pieces(const FewArgs &a, int cols) {
   const int S = a.N * a.K;
   return static_cast<unsigned>((S < a.n_mats ? S : a.n_mats) + S / cols);
+}
+
+// shared_slots_kernel holds a lane's place in x in 32 bits, and wants a workgroup (rows x cols slots) for every CU
+bool shared_takes(const FewArgs &a, int rows, int cols) {
+  return static_cast<int64_t>(a.x_by_slot ? a.N * a.K : a.N) * a.cols * 2 < (1ll << 32) && a.rows / rows * most_pieces(a, cols) >= 256;
 }
 
 template <typename T, int G, bool SWIGLU, int RT, int TT, int WAVES>
@@ -897,9 +899,16 @@ void launch_shared(const FewArgs &a, hipStream_t s) {
 //  many slots an expert  shared_slots_kernel where the weights are no longer most of what comes into a CU.  Gate | up, 4 bits:
 //                        32 slots 29.5 against 39.8, 16 24.4 against 27.4, 8 21.5 against 18.8.  bf16: 32 slots 70 + 41 against
 //                        92 + 57, 4 67 + 38 against 55 + 29.  Not the 4-bit projection (32 slots 23.7 against 28.9).
-//  else                  many_slots_kernel: few row tiles in short calls (enough workgroups), more in long ones (less of x):
-//                        the 4-bit projection with 8 wavefronts up to 512 workgroups (4 tokens 6.5 against 8.1), with 4 beyond (64
-//                        tokens 12.5 against 13.6), of four row tiles from 8 slots an expert on (32: 23.7 against 31.5)
+//  else                  many_slots_kernel: few row tiles in short calls (enough workgroups), more in long ones (less of x read);
+//                        eight wavefronts where the contraction is deep and workgroups are few.
+//    4 bits  gate | up: four row tiles from 512 workgroups on (4 tokens 10.2; two: 10.1; 8 tokens 12.7, 14.2), two below (512 x 1024, 64
+//            tokens 5.6; four: 6.4).  Projection: two tiles with eight wavefronts up to 512 workgroups (4 tokens 6.5 against
+//            8.1 with four), with four beyond (64 tokens 12.5 against 13.6); four tiles from 8 slots an expert on (32: 23.7
+//            against 31.5).
+//    bf16    two tiles; the projection up to 4 slots an expert one with eight wavefronts (4: 29 against 37; 8 slots of 1024 x 2048:
+//            12.6 against 11.3).
+//    fp32    two tiles from 512 workgroups on (100 tokens through 4096 x 1024 in 4 bits 21.6 against 27.3), one below (8 tokens of
+//            512 x 1024 9.8 against 10.8), from 2048 columns on with eight wavefronts.
 constexpr int kOneTokenRows = 4096;
 constexpr int kManyAvg = 8;
 
@@ -913,20 +922,23 @@ hipError_t launch_form(const FewArgs &a, hipStream_t s) {
     }
   }
   const int64_t met = S < a.n_mats ? S : a.n_mats;              // experts, at most
-  const bool dense = S > kManyAvg * met;
+  const bool dense = S > kManyAvg * met, deep = a.cols > 1024;  // deep: two blocks and more for each of eight wavefronts
   if constexpr (sizeof(T) == 4) {
-    launch_many<T, G, SWIGLU, 1, 1, 4>(a, s);
+    if (a.rows / 32 * met >= 512) launch_many<T, G, SWIGLU, 2, 1, 4>(a, s);
+    else if (a.cols >= 2048) launch_many<T, G, SWIGLU, 1, 1, 8>(a, s);
+    else launch_many<T, G, SWIGLU, 1, 1, 4>(a, s);
   } else if constexpr (G == 0) {
-    if (dense && shared_takes(a)) launch_shared<G, SWIGLU, 1, 4, 2, 4>(a, s);
-    else if (!SWIGLU && a.rows / 16 * met <= 2048) launch_many<T, G, SWIGLU, 1, 1, 8>(a, s);
+    if (dense && shared_takes(a, 64, 64)) launch_shared<G, SWIGLU, 1, 4, 2, 4>(a, s);
+    else if (!SWIGLU && deep && S <= 4 * met) launch_many<T, G, SWIGLU, 1, 1, 8>(a, s);
     else launch_many<T, G, SWIGLU, 2, 1, 4>(a, s);
   } else if constexpr (SWIGLU) {
-    if (dense && shared_takes(a)) launch_shared<G, SWIGLU, 2, 2, 2, 4>(a, s);
-    else if (a.rows / 64 * met < 512) launch_many<T, G, SWIGLU, 2, 1, 8>(a, s);
-    else launch_many<T, G, SWIGLU, 4, 1, 4>(a, s);
+    if (dense && shared_takes(a, 128, 32)) launch_shared<G, SWIGLU, 2, 2, 2, 4>(a, s);
+    else if (a.rows / 64 * met >= 512) launch_many<T, G, SWIGLU, 4, 1, 4>(a, s);
+    else if (deep && S == 1) launch_many<T, G, SWIGLU, 2, 1, 8>(a, s);
+    else launch_many<T, G, SWIGLU, 2, 1, 4>(a, s);
   } else {
     if (dense) launch_many<T, G, SWIGLU, 4, 1, 4>(a, s);
-    else if (a.rows / 32 * met <= 512) launch_many<T, G, SWIGLU, 2, 1, 8>(a, s);
+    else if (deep && a.rows / 32 * met <= 512) launch_many<T, G, SWIGLU, 2, 1, 8>(a, s);
     else launch_many<T, G, SWIGLU, 2, 1, 4>(a, s);
   }
   if (!SWIGLU && a.K > 1)
