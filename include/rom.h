@@ -501,7 +501,9 @@ ROM_API int rom_q4_project(int dtype, const void *w_q4, int32_t n_mats, int32_t 
  *   expert_idx   i32 [N, K], gate f32 [N, K]: as rom_route, a layer call or a step left them; expert_idx as above
  *   pre_norm, eps, add_skip, x, out   as rom_ffn_moe_forward
  *   ws           rom_ffn_step_workspace_bytes(dims, d_ff, N), 256-byte aligned
- * SiLU(gate) * up is rounded to T between the launches; every sum is fp32.  N at most ROM_FEW_TOKENS. */
+ * SiLU(gate) * up is rounded to T between the launches; every sum is fp32.  N at most ROM_FEW_TOKENS, d_ff at most
+ * 2^19, d_model 2^20.  Repeated calls give identical bits; a token's result does not depend on the other tokens of a call of
+ * the same N.  (bf16 weights read by more than about eight slots an expert are faster through rom_ffn_moe_forward.) */
 ROM_API size_t rom_ffn_step_workspace_bytes(const rom_dims *dims, int32_t d_ff, int64_t N);
 ROM_API int rom_ffn_moe_step(const rom_dims *dims, int32_t d_ff, const rom_ffn_weights *w, int32_t q4_group, int pre_norm,
                              float eps, int add_skip, const void *x, int64_t N, const int32_t *expert_idx,
@@ -522,7 +524,8 @@ ROM_API int rom_block_step_q4(const rom_dims *dims, const rom_weights *w, int32_
 /* One new token per sequence through the hybrid stack of rom_hybrid_stack_forward: x, out, tmp T [B, d_model], the
  * [n_layers, B, ...] states updated in place.  q4_group 0: the weights of rom_hybrid_stack_forward; 32, 64 or
  * 128: w_in, w_out and both FFN weights of every layer are packed by rom_q4_pack with that group (B at most
- * ROM_FEW_TOKENS then).  Every FFN-MoE block runs on the decision of the RoM block in front of it.
+ * ROM_FEW_TOKENS then).  Every FFN-MoE block runs on the decision of the RoM block in front of it: as rom_ffn_moe_step
+ * with q4_group, in fp32 and for bf16 weights that few slots share, otherwise (and beyond ROM_FEW_TOKENS) as rom_ffn_moe_forward.
  *   ws      rom_workspace_bytes(dims, B, 1), with q4_group rom_step_q4_workspace_bytes(dims, B)
  *   ffn_ws  rom_hybrid_step_ffn_workspace_bytes(dims, d_ff, B, q4_group), distinct from ws (may be NULL if no layer has
  *           an FFN) */

@@ -1323,9 +1323,10 @@ int rom_q4_project(int dtype, const void *w_q4, int32_t n_mats, int32_t rows, in
 namespace {
 int check_ffn_step(const rom_dims *d, int32_t d_ff, int32_t q4_group) {
   int rc = check_ffn(d, d_ff);
-  if (rc != ROM_OK || q4_group == 0) return rc;
-  if (!q4_group_ok(q4_group)) return ROM_E_INVAL;
-  if (d_ff > (1 << 19)) return ROM_E_UNSUPPORTED;
+  if (rc != ROM_OK) return rc;
+  if (q4_group != 0 && !q4_group_ok(q4_group)) return ROM_E_INVAL;
+  if (d_ff > (1 << 19) || d->d_model > (1 << 20)) return ROM_E_UNSUPPORTED;      // rows and columns as for 4 bits
+  if (q4_group == 0) return ROM_OK;
   rc = check_q4(d->n_experts, 2 * d_ff, d->d_model, q4_group);
   return rc != ROM_OK ? rc : check_q4(d->n_experts, d->d_model, d_ff, q4_group);
 }
@@ -1339,10 +1340,20 @@ FfnStepPlan make_ffn_step_plan(const rom_dims *d, int32_t d_ff, int64_t N) {
   p.total = p.partial + align_up(few_partial_bytes(d->d_model, d->top_k, N));
   return p;
 }
+// Whether the FFN-MoE block of a hybrid step runs as rom_ffn_moe_step.  bf16 weights read by many slots an expert are better off with
+// the grouped GEMM, as the RoM block has left the grouping: d_model 2048, d_ff 4096, us: 8 experts, 4 tokens 39 against
+// 42, 16 74 / 86, 64 93 / 90, 256 114 / 93; 16 experts top-2, 32 tokens 158 / 164, 64 176 / 164; d_model 1024, 64 tokens 29 / 35, 256
+// 43 / 36.  fp32 (d_model 512) 8 tokens 24 / 42, 256 73 / 92.
+bool hybrid_ffn_by_step(const rom_dims *d, int64_t B, int32_t q4_group) {
+  if (q4_group) return true;                             // B was checked
+  if (B > ROM_FEW_TOKENS) return false;
+  const int64_t S = B * d->top_k, met = S < d->n_experts ? S : d->n_experts;
+  return d->dtype == ROM_DTYPE_F32 || S <= 8 * met;
+}
 }  // namespace
 
 size_t rom_ffn_step_workspace_bytes(const rom_dims *dims, int32_t d_ff, int64_t N) {
-  if (check_ffn(dims, d_ff) != ROM_OK || N < 0 || N > ROM_FEW_TOKENS) return 0;
+  if (check_ffn_step(dims, d_ff, 0) != ROM_OK || N < 0 || N > ROM_FEW_TOKENS) return 0;
   return make_ffn_step_plan(dims, d_ff, N > 0 ? N : 1).total;
 }
 
@@ -1405,9 +1416,9 @@ int rom_block_step_q4(const rom_dims *dims, const rom_weights *w, int32_t q4_gro
 size_t rom_hybrid_step_ffn_workspace_bytes(const rom_dims *dims, int32_t d_ff, int64_t B, int32_t q4_group) {
   if (check_ffn_step(dims, d_ff, q4_group) != ROM_OK || B < 0 || (q4_group && B > ROM_FEW_TOKENS)) return 0;
   const int64_t n = B > 0 ? B : 1;
-  // room for a call is room for a smaller one: those of at most ROM_FEW_TOKENS run as rom_ffn_moe_step
+  // room for a call is room for a smaller one, which may run the other way (hybrid_ffn_by_step)
   const size_t few = make_ffn_step_plan(dims, d_ff, n < ROM_FEW_TOKENS ? n : ROM_FEW_TOKENS).total;
-  const size_t many = n > ROM_FEW_TOKENS ? make_ffn_plan(dims, d_ff, n).total : 0;
+  const size_t many = q4_group ? 0 : make_ffn_plan(dims, d_ff, n).total;
   return few > many ? few : many;
 }
 
@@ -1457,7 +1468,7 @@ int rom_hybrid_stack_step(const rom_dims *dims, int32_t d_ff, const rom_block *b
     src = dst;
     if (!ffns[j].w_gate_up) continue;
     dst = next_dst();                   // the routing decision is where the RoM block has just left it
-    if (B <= ROM_FEW_TOKENS)
+    if (hybrid_ffn_by_step(dims, B, q4_group))
       rc = rom_ffn_moe_step(dims, d_ff, &ffns[j], q4_group, ffn_pre_norm, eps, 1, src, B,
                             reinterpret_cast<const int32_t *>(base + p.expert_idx), reinterpret_cast<const float *>(base + p.gate),
                             dst, ffn_ws, ffn_ws_bytes, hip_stream);

@@ -101,6 +101,29 @@ def test_pack_a_whole_layers_weight():
         assert np.array_equal(np64(q.unpack(torch.float32)[e, r]), F.q4_values(codes, scales, 64)[0, 0])
 
 
+def test_pack_of_every_quotient_of_two_bf16_numbers():
+    """Every mantissa of a scale with every bf16 size from 6 s down to 2^-4 s: the code is the one that 64 bits choose."""
+    s = (torch.arange(128, 256, device=DEV, dtype=torch.float64) / 128)
+    w = torch.arange(128, 256, device=DEV, dtype=torch.float64).repeat(8) * 2.0 ** torch.arange(-11, -3, device=DEV).repeat_interleave(128)
+    groups = []
+    for part in w.view(-1, 16):                             # 16 sizes, their negatives' mirror and the group's largest
+        top = (6 * s).to(torch.bfloat16).double()           # 6 s rounded: its sixth is s again where that is representable
+        v = torch.where(part[None, :] <= top[:, None], part[None, :], torch.zeros_like(part)[None, :])
+        groups.append(torch.cat([top[:, None], v, -v[:, :15]], dim=1))
+    w3 = torch.stack(groups, 1).reshape(1, 128, -1).to(torch.bfloat16)
+    q = RomQ4Weight.pack(w3, 32)
+    got = q.unpack(torch.float32).double().view(128, -1, 32)
+    v = w3.double().view(128, -1, 32)
+    scale = (v.abs().amax(-1, keepdim=True) / 6).float().to(torch.bfloat16).double()
+    table = torch.tensor(F.E2M1, device=DEV)
+    a = v.abs().unsqueeze(-1)
+    # the nearest; on a tie (both distances exact in 64 bits) the even code
+    d = (a - table * scale.unsqueeze(-1)).abs()
+    best = d.amin(-1, keepdim=True)
+    code = torch.where((d == best) & (torch.arange(8, device=DEV) % 2 == 0), 0, torch.where(d == best, 1, 2)).argmin(-1)
+    assert torch.equal(got, torch.sign(v) * table[code] * scale)
+
+
 # ---------------------------------------------------------------- routed projection
 
 
@@ -188,6 +211,21 @@ def test_project_gives_the_same_bits_again(N, K):
     want = q.project(x, idx, gate)
     for _ in range(3):
         assert torch.equal(q.project(x, idx, gate), want)
+
+
+@pytest.mark.parametrize("N,K,dtype", [(12, 1, "bf16"), (12, 2, "bf16"), (200, 1, "bf16"), (12, 2, "fp32")])
+def test_a_token_does_not_depend_on_the_others(N, K, dtype):
+    cfg, layer, ffn = ffn_holder(192, 320, 4, K, dtype)
+    q, _ = q4_of(3, 4, 64, 192, 64)
+    x, (idx, gate) = randn(4, N, 192, dtype=dtype), routing(5, N, K, 4)
+    other, (idx2, gate2) = randn(6, N, 192, dtype=dtype), routing(7, N, K, 4)
+    keep = torch.arange(0, N, 3, device=DEV)
+    to = keep.flip(0)                                       # the same tokens elsewhere, among others
+    other[to], idx2[to], gate2[to] = x[keep], idx[keep], gate[keep]
+    assert torch.equal(q.project(x, idx, gate)[keep], q.project(other, idx2, gate2)[to])
+    for group in (0, 64):
+        a, b = ffn.step(x, idx, gate, True, True, group), ffn.step(other, idx2, gate2, True, True, group)
+        assert torch.equal(a[keep], b[to])
 
 
 def test_project_refuses_what_does_not_fit():
@@ -363,7 +401,8 @@ def hybrid(cfg, n_layers=3, f=96, holes=(1,)):
 
 
 @pytest.mark.parametrize("group", [0, 64])
-@pytest.mark.parametrize("kw", [dict(), dict(batch=1, top_k=2, gate_mode=1), dict(batch=40), dict(dtype="fp32", batch=2)])
+@pytest.mark.parametrize("kw", [dict(), dict(batch=1, top_k=2, gate_mode=1), dict(batch=20), dict(batch=40), dict(dtype="fp32", batch=2),
+                                dict(dtype="fp32", batch=50)])
 def test_hybrid_step_is_the_calls_one_by_one(kw, group):
     cfg = step_cfg(**kw)
     stack = hybrid(cfg)
@@ -375,8 +414,14 @@ def test_hybrid_step_is_the_calls_one_by_one(kw, group):
         h = x
         for j, (layer, ffn) in enumerate(zip(stack.layers, stack.ffns)):
             h = layer.block_step_q4(h, cs1[j], ss1[j], group) if group else layer.block_step(h, cs1[j], ss1[j])
-            if ffn is not None:
+            slots = cfg.batch * cfg.top_k
+            if ffn is None:
+                continue
+            if group or cfg.dtype == "fp32" or slots <= 8 * min(slots, cfg.n_experts):
                 h = ffn.step(h, layer.ws_view("expert_idx", cfg.batch, 1), layer.ws_view("gate", cfg.batch, 1), True, True, group)
+            else:
+                routing = {n: layer.ws_view(n, cfg.batch, 1) for n in ("offsets", "perm", "inv_perm", "gate")}
+                h = ffn.forward(h, routing, True, True)
         assert torch.equal(got, h) and torch.equal(cs, cs1) and torch.equal(ss, ss1)
 
 
@@ -437,6 +482,32 @@ def test_hybrid_step_replayed_from_a_graph(kw, group):
         got = out.clone()
         want = stack.step(x, want_cs, want_ss, group)
         assert torch.equal(got, want) and torch.equal(cs, want_cs) and torch.equal(ss, want_ss)
+
+
+def test_two_graphs_of_one_holder_replayed_in_turn():
+    """Calls of different sizes of the same holders captured into two graphs: they share a workspace and follow each other."""
+    cfg, layer, ffn = ffn_holder(128, 256, 8, 2, "bf16")
+    q, _ = q4_of(3, 8, 256, 128, 64)
+    sets = []
+    for N in (30, 3):
+        x, (idx, gate) = randn(N, N, 128), routing(N, N, 2, 8)
+        ffn.step(x, idx, gate, True, True, 64), q.project(x, idx, gate)
+        out, out2 = torch.empty_like(x), torch.empty((N, 256), dtype=x.dtype, device=DEV)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            ffn.step(x, idx, gate, True, True, 64, out)
+            q.project(x, idx, gate, out=out2)
+        sets.append((g, x, idx, gate, out, out2))
+    for t in range(4):
+        for g, x, idx, gate, out, out2 in sets:
+            x.copy_(randn(100 + t, *x.shape))
+            idx.copy_(routing(t, x.shape[0], 2, 8)[0])
+        for g, *_ in sets:
+            g.replay()
+        torch.cuda.synchronize()
+        for g, x, idx, gate, out, out2 in sets:
+            assert torch.equal(out, ffn.step(x, idx, gate, True, True, 64)) and torch.equal(out2, q.project(x, idx, gate))
 
 
 def test_two_holders_on_two_streams():
