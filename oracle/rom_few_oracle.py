@@ -67,6 +67,7 @@ def project(x, w, idx, gate=None, row_scale=None, residual=None):
     """(out [N, rows], size of the terms [N, rows]); x [N, cols] or [N, K, cols]; idx [N, K]."""
     x, w = np.asarray(x, F64), np.asarray(w, F64)
     N, K = idx.shape
+    w_size = np.abs(w)
     out, size = np.zeros((N, w.shape[1])), np.zeros((N, w.shape[1]))
     for n in range(N):
         for k in range(K):
@@ -76,7 +77,7 @@ def project(x, w, idx, gate=None, row_scale=None, residual=None):
             v = x[n, k] if x.ndim == 3 else x[n]
             g = 1.0 if gate is None else float(gate[n, k])
             out[n] += g * (w[e] @ v)
-            size[n] += abs(g) * (np.abs(w[e]) @ np.abs(v))
+            size[n] += abs(g) * (w_size[e] @ np.abs(v))
     if row_scale is not None:
         out, size = out * np.asarray(row_scale, F64)[:, None], size * np.abs(np.asarray(row_scale, F64))[:, None]
     return (out if residual is None else out + np.asarray(residual, F64)), size
@@ -90,6 +91,7 @@ def ffn_step(x, w_gate_up, w_down, idx, gate, pre_norm, eps, skip):
     x, wg, wd = np.asarray(x, F64), np.asarray(w_gate_up, F64), np.asarray(w_down, F64)
     N, K = idx.shape
     f = wg.shape[1] // 2
+    wg_size, wd_size = np.abs(wg), np.abs(wd)
     xn = x / np.sqrt(np.mean(x * x, -1, keepdims=True) + eps) if pre_norm else x
     out, size, carried = np.zeros_like(x), np.zeros_like(x), np.zeros_like(x)
     for n in range(N):
@@ -98,10 +100,10 @@ def ffn_step(x, w_gate_up, w_down, idx, gate, pre_norm, eps, skip):
             if e < 0 or e >= wg.shape[0]:
                 continue
             a, b = wg[e, :f] @ xn[n], wg[e, f:] @ xn[n]
-            sa, sb = np.abs(wg[e, :f]) @ np.abs(xn[n]), np.abs(wg[e, f:]) @ np.abs(xn[n])
+            sa, sb = wg_size[e, :f] @ np.abs(xn[n]), wg_size[e, f:] @ np.abs(xn[n])
             s = a / (1.0 + np.exp(-a))
             g = float(gate[n, k])
             out[n] += g * (wd[e] @ (s * b))
-            size[n] += abs(g) * (np.abs(wd[e]) @ np.abs(s * b))
-            carried[n] += abs(g) * (np.abs(wd[e]) @ (1.1 * sa * np.abs(b) + np.abs(s) * sb + np.abs(s * b) * (np.abs(a) + 4)))
+            size[n] += abs(g) * (wd_size[e] @ np.abs(s * b))
+            carried[n] += abs(g) * (wd_size[e] @ (1.1 * sa * np.abs(b) + np.abs(s) * sb + np.abs(s * b) * (np.abs(a) + 4)))
     return (out + x if skip else out), size, carried

@@ -153,7 +153,8 @@ def check_project(q, values, x, idx, gate, row_scale, residual, dtype):
     (8, 1, 8, 72, 520, 64, "random"), (5, 1, 3, 16, 128, 128, "missing"), (2, 4, 4, 56, 1000, 64, "again"), (4, 2, 2, 8, 3000, 32, "one"),
     (9, 1, 8, 64, 256, 64, "random"), (5, 2, 4, 40, 136, 32, "missing"), (16, 2, 16, 72, 264, 64, "random"), (17, 1, 4, 136, 520, 128, "one"),
     (33, 8, 64, 24, 96, 32, "random"), (64, 2, 3, 48, 200, 64, "again"), (256, 1, 8, 64, 384, 32, "random"), (256, 8, 16, 32, 128, 128, "missing"),
-    (100, 1, 64, 16, 640, 64, "random"), (255, 2, 2, 24, 72, 64, "random"), (40, 1, 5, 200, 2048, 64, "missing")])
+    (100, 1, 64, 16, 640, 64, "random"), (1, 2, 8, 4104, 136, 64, "random"), (1, 1, 4, 4104, 1160, 128, "random"),
+    (1, 2, 4, 4104, 72, 32, "missing"), (255, 2, 2, 24, 72, 64, "random"), (40, 1, 5, 200, 2048, 64, "missing")])
 def test_project(dtype, N, K, E, rows, cols, group, kind):
     q, values = q4_of(rows + cols, E, rows, cols, group)
     x = randn(N + cols, N, cols, dtype=dtype)
@@ -264,6 +265,20 @@ FFN_CASES = [
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("N,K,E,D,f,kind,norm", FFN_CASES)
 def test_ffn_moe_step(dtype, group, N, K, E, D, f, kind, norm):
+    check_ffn(dtype, group, N, K, E, D, f, kind, norm)
+
+
+# sizes at which the calls take each of the other forms: many slots an expert, many and few row tiles, deep contractions
+@pytest.mark.parametrize("dtype,group,N,K,E,D,f,kind,norm", [
+    ("bf16", 64, 256, 1, 4, 328, 1424, "missing", 1), ("bf16", 32, 130, 2, 4, 200, 1424, "random", 1), ("bf16", 128, 140, 1, 2, 72, 2064, "one", 0),
+    ("bf16", 128, 64, 1, 64, 72, 272, "random", 1), ("bf16", 64, 1, 1, 4, 1160, 48, "random", 1), ("bf16", 64, 9, 2, 4, 136, 2064, "random", 1),
+    ("bf16", 0, 256, 1, 4, 200, 1040, "missing", 1), ("bf16", 0, 200, 2, 4, 2056, 48, "random", 0), ("bf16", 0, 9, 1, 8, 72, 1168, "random", 1),
+    ("fp32", 0, 64, 1, 64, 264, 144, "random", 1), ("fp32", 64, 64, 1, 64, 264, 144, "random", 1), ("fp32", 0, 9, 1, 4, 2056, 32, "missing", 1)])
+def test_ffn_moe_step_in_its_other_forms(dtype, group, N, K, E, D, f, kind, norm):
+    check_ffn(dtype, group, N, K, E, D, f, kind, norm)
+
+
+def check_ffn(dtype, group, N, K, E, D, f, kind, norm):
     gu, down = randn(D, E, 2 * f, D, std=1.5 * D ** -0.5, dtype=dtype), randn(f, E, D, f, std=f ** -0.5, dtype=dtype)
     x = randn(N, N, D, std=1.7, dtype=dtype)
     idx, gate = routing(N + K, N, K, E, kind)
