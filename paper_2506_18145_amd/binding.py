@@ -606,6 +606,12 @@ def _keep_if_captured(kept: list, *buffers) -> None:
         kept.extend(b for b in buffers if b is not None and not any(b is k for k in kept))
 
 
+def _not_while_capturing(what: str) -> None:
+    """What a holder lays out once would, under capture, be laid out by the graph's replays only."""
+    if torch.cuda.is_current_stream_capturing():
+        raise RomError(f"{what} has to be called once before a capture: it packs the weights")
+
+
 _TORCH_TYPE = {ROM_DTYPE_F32: torch.float32, ROM_DTYPE_BF16: torch.bfloat16}
 
 
@@ -619,6 +625,19 @@ def _dtype_code(dtype) -> int:
 
 def rom_q4_bytes(n_mats: int, rows: int, cols: int, group: int) -> int:
     return int(load_library().rom_q4_bytes(n_mats, rows, cols, group))
+
+
+def _weight_bytes(n_mats: int, rows: int, cols: int, group: int, element_size: int) -> int:
+    """Bytes of a stack, plain (group 0) or in 4 bits."""
+    if group == 0:
+        return n_mats * rows * cols * element_size
+    codes = n_mats * (-(-rows // 16) * 16) * (-(-cols // 128) * 128) // 2
+    return codes + 4 * codes // group
+
+
+def _expect_weight(t: torch.Tensor, what: str, need: int, index: int) -> None:
+    if t.numel() * t.element_size() != need or t.get_device() != index or not t.is_contiguous():
+        raise RomError(f"{what}: expected {need} contiguous bytes on cuda:{index}, got {t.numel() * t.element_size()} on {t.device}")
 
 
 def rom_q4_pack(w: torch.Tensor, group: int, w_q4: torch.Tensor) -> None:
@@ -655,6 +674,8 @@ def rom_q4_project(w_q4, n_mats, rows, cols, group, x, expert_idx, gate, row_sca
     _expect(row_scale, "row_scale", torch.float32, (n,), index)
     _expect(residual, "residual", dtype, (n, rows), index)
     _expect(out, "out", dtype, (n, rows), index)
+    if group > 0:
+        _expect_weight(w_q4, "w_q4", _weight_bytes(n_mats, rows, cols, group, 1), index)
     code = load_library().rom_q4_project(
         _dtype_code(dtype), w_q4.data_ptr(), n_mats, rows, cols, group, x.data_ptr(), n, k, _at(expert_idx), _at(gate),
         _at(row_scale), _at(residual), out.data_ptr(), _at(ws), _nbytes(ws), _raw_stream(index))
@@ -672,6 +693,9 @@ def rom_ffn_moe_step(dims, d_ff, w_gate_up, w_down, q4_group, pre_norm, eps, add
     _expect(out, "out", dtype, (n_tokens, dims.d_model), index)
     _expect(expert_idx, "expert_idx", torch.int32, (n_tokens, k), index)
     _expect(gate, "gate", torch.float32, (n_tokens, k), index)
+    size = x.element_size()
+    _expect_weight(w_gate_up, "w_gate_up", _weight_bytes(dims.n_experts, 2 * d_ff, dims.d_model, q4_group, size), index)
+    _expect_weight(w_down, "w_down", _weight_bytes(dims.n_experts, dims.d_model, d_ff, q4_group, size), index)
     w = _RomFfnWeights(w_gate_up.data_ptr(), w_down.data_ptr())
     code = load_library().rom_ffn_moe_step(
         ctypes.byref(dims), d_ff, ctypes.byref(w), q4_group, 1 if pre_norm else 0, eps, 1 if add_skip else 0, x.data_ptr(),
@@ -792,6 +816,7 @@ class RomLayer:
         """The parameters step_q4 (block: block_step_q4, the pre-norm's scale folded in first) takes: w_in and w_out
         in 4 bits, packed once, everything else shared with the plain layer."""
         if (group, block) not in self._q4:
+            _not_while_capturing("q4_weights")
             w = dict(self.block_weights() if block else self.weights)
             w["w_in"] = RomQ4Weight.pack(w["w_in"], group).packed
             w["w_out"] = RomQ4Weight.pack(w["w_out"], group).packed
@@ -1105,6 +1130,7 @@ class RomFfnMoe:
     def q4_weights(self, group: int, pre_norm: bool):
         """(gate | up in the library's row order, down), both in 4 bits, packed once."""
         if (group, bool(pre_norm)) not in self._q4:
+            _not_while_capturing("q4_weights")
             pack = lambda w: RomQ4Weight.pack(w, group).packed
             self._q4[(group, bool(pre_norm))] = (pack(self.packed(bool(pre_norm))), pack(self.w_down))
         return self._q4[(group, bool(pre_norm))]

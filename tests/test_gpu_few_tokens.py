@@ -356,6 +356,13 @@ def test_ffn_step_refuses_what_does_not_fit():
             ffn.step(a["x"], a["idx"], a["gate"], q4_group=a["q4_group"], out=a["out"])
     with pytest.raises(RomError):
         ffn.step(randn(1, 257, 64), *routing(2, 257, 2, 4))
+    ws, out = torch.empty(rom_ffn_step_workspace_bytes(ffn.dims, 32, 3), dtype=torch.uint8, device=DEV), torch.empty_like(x)
+    gu, down = ffn.packed(False), ffn.w_down
+    for bad in (dict(gu=gu[:3]), dict(down=down.float()), dict(group=32), dict(ws=ws[:-1])):
+        a = dict(gu=gu, down=down, group=0, ws=ws)
+        a.update(bad)
+        with pytest.raises(RomError):
+            rom_ffn_moe_step(ffn.dims, 32, a["gu"], a["down"], a["group"], False, 1e-5, False, x, 3, idx, gate, out, a["ws"])
 
 
 # ---------------------------------------------------------------- steps
@@ -497,6 +504,26 @@ def test_hybrid_step_replayed_from_a_graph(kw, group):
         got = out.clone()
         want = stack.step(x, want_cs, want_ss, group)
         assert torch.equal(got, want) and torch.equal(cs, want_cs) and torch.equal(ss, want_ss)
+
+
+def test_weights_are_not_packed_by_a_capture():
+    cfg, layer, ffn = ffn_holder(64, 32, 4, 1, "bf16")
+    x, (idx, gate) = randn(1, 3, 64), routing(2, 3, 1, 4)
+    cs, ss = randn(1, 3, 128, 3, dtype="fp32"), randn(2, 3, 128, 16, dtype="fp32")
+    want = ffn.step(x, idx, gate)                               # plain weights: nothing to lay out
+    refused = []
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = ffn.step(x, idx, gate)
+        for call in (lambda: ffn.step(x, idx, gate, q4_group=32), lambda: layer.step_q4(x, cs, ss, 32)):
+            try:
+                call()
+            except RomError as e:
+                refused.append("before a capture" in str(e))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert refused == [True, True] and torch.equal(out, want)
+    assert bool(torch.isfinite(ffn.step(x, idx, gate, q4_group=32)).all())
 
 
 def test_two_graphs_of_one_holder_replayed_in_turn():
