@@ -520,16 +520,16 @@ __device__ __forceinline__ bool find_piece(const FewArgs &a, int row0, Pieces<CO
   return true;
 }
 
-// Short calls: a workgroup owns RT row tiles of 16 for up to 16 TT slots of one expert; its wavefronts deal the blocks of 128
+// Short calls: a workgroup owns RT row tiles of 16 for up to 16 slots of one expert; its wavefronts deal the blocks of 128
 // columns among themselves, and their sums meet in LDS.  Bound by the lines that a CU's L1 can have under way: 32 tokens in 4
 // bits, d_model 2048, d_ff 4096: 75 MB in 19.0 us, 38 MB in 11.9, of which 3.5 are the launch, the routing decision and the last sums.
 // No block is requested ahead of the last one's products: other wavefronts do that, and requests past a short row's end cost more than
 // they hide (3 to 30 % at every size).  The register budget of four wavefronts a SIMD for two row tiles and more: left to
 // itself the compiler aims at eight and moves values to accumulator registers and back (16 tokens' gate | up 26.9 us, 16.3 with
 // it); with one row tile eight fit (8 tokens top-2, down projection of 2048 x 1024: 15.6, 13.0).
-template <typename T, int G, bool SWIGLU, int RT, int TT, int WAVES>
+template <typename T, int G, bool SWIGLU, int RT, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, RT >= 2 ? 4 : 8))) void many_slots_kernel(const FewArgs a) {
-  constexpr int ROWS = 16 * RT, COLS = 16 * TT;
+  constexpr int ROWS = 16 * RT, COLS = 16;
   __shared__ __attribute__((aligned(16))) float red[WAVES][COLS][ROWS + 4];
   __shared__ float sq[WAVES][COLS];
   __shared__ Pieces<COLS> sh;
@@ -541,27 +541,18 @@ __global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, R
 
   const int c = lane & 15, q = lane >> 4;
   const Matrix<T, G> m(a, e);
-  const T *x[TT];
+  const int my_slot = slots[c < n_cols ? c : 0];                  // past the end: read again, not stored
+  const T *x = static_cast<const T *>(a.x) + static_cast<int64_t>(a.x_by_slot ? my_slot : my_slot / a.K) * a.cols;
+  f32x4_t acc[RT];
 #pragma unroll
-  for (int t = 0; t < TT; ++t) {
-    const int slot = slots[16 * t + c < n_cols ? 16 * t + c : 0];          // past the end: read again, not stored
-    x[t] = static_cast<const T *>(a.x) + static_cast<int64_t>(a.x_by_slot ? slot : slot / a.K) * a.cols;
-  }
-  f32x4_t acc[RT][TT];
-  float squares[TT];
-#pragma unroll
-  for (int t = 0; t < TT; ++t) {
-    squares[t] = 0.0f;
-#pragma unroll
-    for (int i = 0; i < RT; ++i) acc[i][t] = kZero4;
-  }
+  for (int i = 0; i < RT; ++i) acc[i] = kZero4;
+  float squares = 0.0f;
   for (int b = wave; b < m.col_blocks; b += WAVES) {
-    Eight<T> v[TT][4];
+    Eight<T> v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int k = 128 * b + 32 * j + 8 * q;
-#pragma unroll
-      for (int t = 0; t < TT; ++t) v[t][j].load(x[t] + (k < a.cols ? k : 0));
+      v[j].load(x + (k < a.cols ? k : 0));
     }
     if constexpr (G == 0) {
       Eight<T> w[RT][4];
@@ -577,13 +568,11 @@ __global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, R
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const bool ok = 128 * b + 32 * j + 8 * q < a.cols;
-#pragma unroll
-        for (int t = 0; t < TT; ++t) v[t][j].zero_unless(ok);
+        v[j].zero_unless(ok);
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
           w[i][j].zero_unless(ok);
-#pragma unroll
-          for (int t = 0; t < TT; ++t) acc[i][t] = mma(w[i][j], v[t][j], acc[i][t]);
+          acc[i] = mma(w[i][j], v[j], acc[i]);
         }
       }
     } else {
@@ -597,43 +586,32 @@ __global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, R
         scale[i] = m.scale4(tile, b, 4 * q);
       }
 #pragma unroll
-      for (int t = 0; t < TT; ++t)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[t][j].zero_unless(128 * b + 32 * j + 8 * q < a.cols);
+      for (int j = 0; j < 4; ++j) v[j].zero_unless(128 * b + 32 * j + 8 * q < a.cols);
 #pragma unroll
       for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
-          f32x4_t d[TT];
-#pragma unroll
-          for (int t = 0; t < TT; ++t) d[t] = kZero4;
+          f32x4_t d = kZero4;
 #pragma unroll
           for (int j = g * (4 / GROUPS); j < (g + 1) * (4 / GROUPS); ++j) {
             Eight<T> codes;
             codes.codes(w[i][j]);
-#pragma unroll
-            for (int t = 0; t < TT; ++t) d[t] = mma(codes, v[t][j], d[t]);
+            d = mma(codes, v[j], d);
           }
-#pragma unroll
-          for (int t = 0; t < TT; ++t) acc[i][t] = scaled_add(acc[i][t], d[t], quad_lane(scale[i], g));
+          acc[i] = scaled_add(acc[i], d, quad_lane(scale[i], g));
         }
     }
     if constexpr (SWIGLU) {
 #pragma unroll
-      for (int t = 0; t < TT; ++t)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) squares[t] = square_sum(v[t][j], squares[t]);
+      for (int j = 0; j < 4; ++j) squares = square_sum(v[j], squares);
     }
   }
 #pragma unroll
-  for (int t = 0; t < TT; ++t) {
-#pragma unroll
-    for (int i = 0; i < RT; ++i) *reinterpret_cast<f32x4_t *>(&red[wave][16 * t + c][16 * i + 4 * q]) = acc[i][t];
-    if constexpr (SWIGLU) {
-      squares[t] += __shfl_xor(squares[t], 16);
-      squares[t] += __shfl_xor(squares[t], 32);
-      if (q == 0) sq[wave][16 * t + c] = squares[t];
-    }
+  for (int i = 0; i < RT; ++i) *reinterpret_cast<f32x4_t *>(&red[wave][c][16 * i + 4 * q]) = acc[i];
+  if constexpr (SWIGLU) {
+    squares += __shfl_xor(squares, 16);
+    squares += __shfl_xor(squares, 32);
+    if (q == 0) sq[wave][c] = squares;
   }
   __syncthreads();
   const auto total = [&](int col, int r) __attribute__((always_inline)) {
@@ -678,12 +656,15 @@ __device__ __forceinline__ V load_at(const void *base, unsigned int offset) {
 }
 
 // Many slots an expert: reading their rows costs each CU more than the weights do, so that they are fetched once for
-// 128 RT rows.  A wavefront owns RT row tiles of 16 and all columns; a block of 128 columns of the piece's rows is in LDS for
-// the eight of them (pitch 272 bytes: the reads of 16 rows touch every bank once), the next block's rows and weights are on
-// their way in registers, one barrier a block.  No sum crosses wavefronts.
-template <int G, bool SWIGLU, int RT, int TT, int DEPTH, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, 4))) void shared_slots_kernel(const FewArgs a) {
-  constexpr int COLS = 16 * TT, ROWS = 16 * RT * WAVES, PITCH = 136, GROUPS = G ? 128 / (G ? G : 1) : 1;
+// 64 RT rows.  A wavefront owns RT row tiles of 16 and all columns; a block of 128 columns of the piece's rows is in LDS for
+// the four of them (pitch 272 bytes: the reads of 16 rows touch every bank once), the next two blocks' rows and weights are on
+// their way in registers, one barrier a block.  No sum crosses wavefronts.  256 tokens, 16 experts, top-2, half of the slots on
+// one, 4 bits: gate | up 51.8 us (67 by many_slots_kernel) for 138 MB of weights, 199 with an expert's further pieces, and 96 of
+// rows; eight wavefronts, four blocks under way, 64 slots and 256 rows were 50 to 78, fewer workgroups fitting a CU.
+constexpr int kSharedWaves = 4;
+template <int G, bool SWIGLU, int RT, int TT>
+__global__ __launch_bounds__(kSharedWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 4))) void shared_slots_kernel(const FewArgs a) {
+  constexpr int WAVES = kSharedWaves, DEPTH = 2, COLS = 16 * TT, ROWS = 16 * RT * WAVES, PITCH = 136, GROUPS = G ? 128 / (G ? G : 1) : 1;
   constexpr int XS = 4 * WAVES, XT = (COLS + XS - 1) / XS;      // slots that are fetched together, that a thread fetches
   __shared__ Pieces<COLS> sh;
   __shared__ __attribute__((aligned(16))) bf16_t xs[2][XS * XT * PITCH];
@@ -887,15 +868,15 @@ bool shared_takes(const FewArgs &a, int rows, int cols) {
   return static_cast<int64_t>(a.x_by_slot ? a.N * a.K : a.N) * a.cols * 2 < (1ll << 32) && a.rows / rows * most_pieces(a, cols) >= 256;
 }
 
-template <typename T, int G, bool SWIGLU, int RT, int TT, int WAVES>
+template <typename T, int G, bool SWIGLU, int RT, int WAVES>
 void launch_many(const FewArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL((many_slots_kernel<T, G, SWIGLU, RT, TT, WAVES>), dim3(blocks_of(a.rows, 16 * RT), most_pieces(a, 16 * TT)),
-                     dim3(WAVES * 64), 0, s, a);
+  hipLaunchKernelGGL((many_slots_kernel<T, G, SWIGLU, RT, WAVES>), dim3(blocks_of(a.rows, 16 * RT), most_pieces(a, 16)), dim3(WAVES * 64), 0, s,
+                     a);
 }
-template <int G, bool SWIGLU, int RT, int TT, int DEPTH, int WAVES>
+template <int G, bool SWIGLU, int RT, int TT>
 void launch_shared(const FewArgs &a, hipStream_t s) {
-  hipLaunchKernelGGL((shared_slots_kernel<G, SWIGLU, RT, TT, DEPTH, WAVES>), dim3(blocks_of(a.rows, 16 * RT * WAVES), most_pieces(a, 16 * TT)),
-                     dim3(WAVES * 64), 0, s, a);
+  hipLaunchKernelGGL((shared_slots_kernel<G, SWIGLU, RT, TT>), dim3(blocks_of(a.rows, 16 * RT * kSharedWaves), most_pieces(a, 16 * TT)),
+                     dim3(kSharedWaves * 64), 0, s, a);
 }
 
 // Which kernel takes a call.  Times in us, kernels alone, d_model 2048, d_ff 4096, 8 experts, top-1 unless another size stands there.
@@ -929,22 +910,22 @@ hipError_t launch_form(const FewArgs &a, hipStream_t s) {
   const int64_t met = S < a.n_mats ? S : a.n_mats;              // experts, at most
   const bool dense = S > kManyAvg * met, deep = a.cols > 1024;  // deep: two blocks and more for each of eight wavefronts
   if constexpr (sizeof(T) == 4) {
-    if (a.rows / 32 * met >= 512) launch_many<T, G, SWIGLU, 2, 1, 4>(a, s);
-    else if (a.cols >= 2048) launch_many<T, G, SWIGLU, 1, 1, 8>(a, s);
-    else launch_many<T, G, SWIGLU, 1, 1, 4>(a, s);
+    if (a.rows / 32 * met >= 512) launch_many<T, G, SWIGLU, 2, 4>(a, s);
+    else if (a.cols >= 2048) launch_many<T, G, SWIGLU, 1, 8>(a, s);
+    else launch_many<T, G, SWIGLU, 1, 4>(a, s);
   } else if constexpr (G == 0) {
-    if (dense && shared_takes(a, 64, 64)) launch_shared<G, SWIGLU, 1, 4, 2, 4>(a, s);
-    else if (!SWIGLU && deep && S <= 4 * met) launch_many<T, G, SWIGLU, 1, 1, 8>(a, s);
-    else launch_many<T, G, SWIGLU, 2, 1, 4>(a, s);
+    if (dense && shared_takes(a, 64, 64)) launch_shared<G, SWIGLU, 1, 4>(a, s);
+    else if (!SWIGLU && deep && S <= 4 * met) launch_many<T, G, SWIGLU, 1, 8>(a, s);
+    else launch_many<T, G, SWIGLU, 2, 4>(a, s);
   } else if constexpr (SWIGLU) {
-    if (dense && shared_takes(a, 128, 32)) launch_shared<G, SWIGLU, 2, 2, 2, 4>(a, s);
-    else if (a.rows / 64 * met >= 512) launch_many<T, G, SWIGLU, 4, 1, 4>(a, s);
-    else if (deep && S == 1) launch_many<T, G, SWIGLU, 2, 1, 8>(a, s);
-    else launch_many<T, G, SWIGLU, 2, 1, 4>(a, s);
+    if (dense && shared_takes(a, 128, 32)) launch_shared<G, SWIGLU, 2, 2>(a, s);
+    else if (a.rows / 64 * met >= 512) launch_many<T, G, SWIGLU, 4, 4>(a, s);
+    else if (deep && S == 1) launch_many<T, G, SWIGLU, 2, 8>(a, s);
+    else launch_many<T, G, SWIGLU, 2, 4>(a, s);
   } else {
-    if (dense) launch_many<T, G, SWIGLU, 4, 1, 4>(a, s);
-    else if (deep && a.rows / 32 * met <= 512) launch_many<T, G, SWIGLU, 2, 1, 8>(a, s);
-    else launch_many<T, G, SWIGLU, 2, 1, 4>(a, s);
+    if (dense) launch_many<T, G, SWIGLU, 4, 4>(a, s);
+    else if (deep && a.rows / 32 * met <= 512) launch_many<T, G, SWIGLU, 2, 8>(a, s);
+    else launch_many<T, G, SWIGLU, 2, 4>(a, s);
   }
   if (!SWIGLU && a.K > 1)
     hipLaunchKernelGGL(few_combine_kernel<T>, dim3(blocks_of(static_cast<int64_t>(a.N) * a.rows, 1024)), dim3(256), 0, s, a);
