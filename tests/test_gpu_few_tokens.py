@@ -365,6 +365,38 @@ def test_ffn_step_refuses_what_does_not_fit():
             rom_ffn_moe_step(ffn.dims, 32, a["gu"], a["down"], a["group"], False, 1e-5, False, x, 3, idx, gate, out, a["ws"])
 
 
+@pytest.mark.parametrize("group", [0, 64])
+def test_weights_beyond_32_bit_offsets(group):
+    """64 experts of 2 x 8192 x 4096: 2^32 gate | up weights; the slots of the last expert against the layer in 64 bits."""
+    E, D, f = 64, 4096, 8192
+    gu, down = torch.zeros((E, 2 * f, D), dtype=torch.bfloat16, device=DEV), torch.zeros((E, D, f), dtype=torch.bfloat16, device=DEV)
+    gu[-1], down[-1] = randn(1, 2 * f, D, std=D ** -0.5), randn(2, D, f, std=f ** -0.5)
+    last = gu[-1:].contiguous(), down[-1:].contiguous()
+    if group:
+        gu, down = RomQ4Weight.pack(gu, group).packed, RomQ4Weight.pack(down, group).packed
+        last = tuple(RomQ4Weight.pack(w, group).unpack(torch.float32) for w in last)
+    rows, w_down = last[0][0].double().view(f // 8, 2, 8, D), last[1][0].double()
+    w_gate, w_up = rows[:, 0].reshape(f, D), rows[:, 1].reshape(f, D)
+    dims, u = RomDims(D, 16, 16, 4, 1, E, 1, E, 1, 0), 2.0 ** -8
+    for N in (1, 3, 70):
+        x, gate, out = randn(N, N, D), torch.ones((N, 1), device=DEV), torch.empty((N, D), dtype=torch.bfloat16, device=DEV)
+        ws = torch.empty(rom_ffn_step_workspace_bytes(dims, f, N), dtype=torch.uint8, device=DEV)
+        idx = torch.full((N, 1), E - 1, dtype=torch.int32, device=DEV)
+        rom_ffn_moe_step(dims, f, gu, down, group, True, 1e-5, True, x, N, idx, gate, out, ws)
+        xd = x.double()
+        xn = xd / (xd.square().mean(-1, keepdim=True) + 1e-5).sqrt()
+        a, b, sa, sb = xn @ w_gate.t(), xn @ w_up.t(), xn.abs() @ w_gate.abs().t(), xn.abs() @ w_up.abs().t()
+        silu = a / (1 + torch.exp(-a))
+        want, size = xd + (silu * b) @ w_down.t(), (silu * b).abs() @ w_down.abs().t()
+        carried = (1.1 * sa * b.abs() + silu.abs() * sb + (silu * b).abs() * (a.abs() + 4)) @ w_down.abs().t()
+        tol = (u * 1.001 + 2.0 ** -24) * want.abs() + u * 1.001 * size + 2.0 ** -24 * ((D + 64) * carried + (f + 64) * size)
+        assert bool(((out.double() - want).abs() <= tol).all())
+        # roundings of 8192 terms do not add up: 1/16 of the bound on h holds a mistake that the worst case would let through
+        assert (out.double() - want).norm().item() <= (u * want.abs() + u * size / 16).norm().item()
+    del gu, down
+    torch.cuda.empty_cache()
+
+
 # ---------------------------------------------------------------- steps
 
 
