@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Dict, Optional
 
@@ -627,6 +628,7 @@ def rom_q4_bytes(n_mats: int, rows: int, cols: int, group: int) -> int:
     return int(load_library().rom_q4_bytes(n_mats, rows, cols, group))
 
 
+@functools.lru_cache(maxsize=None)
 def _weight_bytes(n_mats: int, rows: int, cols: int, group: int, element_size: int) -> int:
     """Bytes of a stack, plain (group 0) or in 4 bits."""
     if group == 0:
@@ -666,16 +668,24 @@ def rom_q4_project_workspace_bytes(rows: int, top_k: int, n_tokens: int) -> int:
 
 def rom_q4_project(w_q4, n_mats, rows, cols, group, x, expert_idx, gate, row_scale, residual, out, ws):
     """x [N, cols], out [N, rows]; top_k is expert_idx's second size (1 without)."""
-    index = _current_index(x)
-    n, k, dtype = x.shape[0], 1 if expert_idx is None else expert_idx.shape[-1], x.dtype
+    if group > 0:                                   # else the library refuses it
+        _expect_weight(w_q4, "w_q4", _weight_bytes(n_mats, rows, cols, group, 1), x.get_device())
+    _q4_project(w_q4, n_mats, rows, cols, group, x, 1 if expert_idx is None else expert_idx.shape[-1], expert_idx, gate, row_scale,
+                residual, out, ws)
+
+
+def _q4_project(w_q4, n_mats, rows, cols, group, x, k, expert_idx, gate, row_scale, residual, out, ws):
+    index, n, dtype = _current_index(x), x.shape[0], x.dtype
     _expect(x, "x", dtype, (n, cols), index)
-    _expect(expert_idx, "expert_idx", torch.int32, (n, k), index)
-    _expect(gate, "gate", torch.float32, (n, k), index)
-    _expect(row_scale, "row_scale", torch.float32, (n,), index)
-    _expect(residual, "residual", dtype, (n, rows), index)
+    if expert_idx is not None:
+        _expect(expert_idx, "expert_idx", torch.int32, (n, k), index)
+    if gate is not None:
+        _expect(gate, "gate", torch.float32, (n, k), index)
+    if row_scale is not None:
+        _expect(row_scale, "row_scale", torch.float32, (n,), index)
+    if residual is not None:
+        _expect(residual, "residual", dtype, (n, rows), index)
     _expect(out, "out", dtype, (n, rows), index)
-    if group > 0:
-        _expect_weight(w_q4, "w_q4", _weight_bytes(n_mats, rows, cols, group, 1), index)
     code = load_library().rom_q4_project(
         _dtype_code(dtype), w_q4.data_ptr(), n_mats, rows, cols, group, x.data_ptr(), n, k, _at(expert_idx), _at(gate),
         _at(row_scale), _at(residual), out.data_ptr(), _at(ws), _nbytes(ws), _raw_stream(index))
@@ -776,8 +786,8 @@ class RomQ4Weight:
         if k not in self._ws:
             need = rom_q4_project_workspace_bytes(self.rows, k, ROM_FEW_TOKENS)
             self._ws[k] = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
-        rom_q4_project(self.packed, self.n_mats, self.rows, self.cols, self.group, x, expert_idx, gate, row_scale, residual, out,
-                       self._ws[k])
+        _q4_project(self.packed, self.n_mats, self.rows, self.cols, self.group, x, k, expert_idx, gate, row_scale, residual, out,
+                    self._ws[k])
         return out
 
 
