@@ -520,9 +520,59 @@ __device__ __forceinline__ bool find_piece(const FewArgs &a, int row0, Pieces<CO
   return true;
 }
 
+// position of the n-th (from 0) set bit
+__device__ __forceinline__ int nth_bit(unsigned long long mask, int n) {
+  const unsigned int lo = static_cast<unsigned int>(mask), hi = static_cast<unsigned int>(mask >> 32);
+  const int in_lo = __popc(lo);
+  unsigned int w = n < in_lo ? lo : hi;
+  int at = n < in_lo ? 0 : 32;
+  n -= n < in_lo ? 0 : in_lo;
+#pragma unroll
+  for (int s = 16; s >= 1; s >>= 1) {
+    const int below = __popc(w & ((1u << s) - 1));
+    const bool up = n >= below;
+    n -= up ? below : 0;
+    w = up ? w >> s : w;
+    at += up ? s : 0;
+  }
+  return at;
+}
+
+// The same for up to 64 slots, a lane each, without LDS and barriers: every wavefront by itself, expert after expert in the order in
+// which the slots name them.  0.5 to 1 us of every launch (one token's gate | up in 4 bits 6.2 -> 5.7), 1.6 of 8 tokens top-2's down projection
+// (12.9 -> 11.3).  my_slot: of column lane % 16 (past the end: of the first column).
+template <typename T, bool SWIGLU, int ROWS>
+__device__ __forceinline__ bool find_piece_64(const FewArgs &a, int row0, int &e, int &n_cols, int &my_slot) {
+  const int lane = threadIdx.x & 63, S = a.N * a.K;
+  int v = lane < S && a.expert_idx ? a.expert_idx[lane] : 0;
+  v = lane < S && v >= 0 && v < a.n_mats ? v : -1;
+  unsigned long long left = __ballot(v >= 0);
+  if constexpr (!SWIGLU) {
+    if (a.K == 1 && blockIdx.y == 0) {
+      for (unsigned long long none = __ballot(lane < S) & ~left; none; none &= none - 1)
+        for (int r = threadIdx.x; r < ROWS && row0 + r < a.rows; r += blockDim.x) few_store<T>(a, __builtin_ctzll(none), row0 + r, 0.0f);
+    }
+  }
+  int piece = blockIdx.y;
+  while (left) {
+    e = __builtin_amdgcn_readlane(v, __builtin_ctzll(left));
+    const unsigned long long same = __ballot(v == e);
+    const int pieces = (__popcll(same) + 15) / 16;
+    if (piece < pieces) {
+      const int n = __popcll(same) - 16 * piece, c = lane & 15;
+      n_cols = n < 16 ? n : 16;
+      my_slot = nth_bit(same, 16 * piece + (c < n_cols ? c : 0));
+      return true;
+    }
+    piece -= pieces;
+    left &= ~same;
+  }
+  return false;
+}
+
 // Short calls: a workgroup owns RT row tiles of 16 for up to 16 slots of one expert; its wavefronts deal the blocks of 128
 // columns among themselves, and their sums meet in LDS.  Bound by the lines that a CU's L1 can have under way: 32 tokens in 4
-// bits, d_model 2048, d_ff 4096: 75 MB in 19.0 us, 38 MB in 11.9, of which 3.5 are the launch, the routing decision and the last sums.
+// bits, d_model 2048, d_ff 4096: 75 MB in 18.9 us, 38 MB in 11.4, of which 3 are the launch, the routing decision and the last sums.
 // No block is requested ahead of the last one's products: other wavefronts do that, and requests past a short row's end cost more than
 // they hide (3 to 30 % at every size).  The register budget of four wavefronts a SIMD for two row tiles and more: left to
 // itself the compiler aims at eight and moves values to accumulator registers and back (16 tokens' gate | up 26.9 us, 16.3 with
@@ -535,13 +585,17 @@ __global__ __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(2, R
   __shared__ Pieces<COLS> sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int row0 = blockIdx.x * ROWS;
-  int e, n_cols;
-  if (!find_piece<T, SWIGLU, COLS, ROWS>(a, row0, sh, e, n_cols)) return;
-  const int *slots = sh.slots;
-
   const int c = lane & 15, q = lane >> 4;
+  int e, n_cols, my_slot;                                         // my_slot: of column c, past the end of the first: read again, not stored
+  if (a.N * a.K <= 64) {
+    if (!find_piece_64<T, SWIGLU, ROWS>(a, row0, e, n_cols, my_slot)) return;
+    if (tid < n_cols) sh.slots[tid] = my_slot;                    // read behind the barrier that the sums wait at
+  } else {
+    if (!find_piece<T, SWIGLU, COLS, ROWS>(a, row0, sh, e, n_cols)) return;
+    my_slot = sh.slots[c < n_cols ? c : 0];
+  }
+  const int *slots = sh.slots;
   const Matrix<T, G> m(a, e);
-  const int my_slot = slots[c < n_cols ? c : 0];                  // past the end: read again, not stored
   const T *x = static_cast<const T *>(a.x) + static_cast<int64_t>(a.x_by_slot ? my_slot : my_slot / a.K) * a.cols;
   f32x4_t acc[RT];
 #pragma unroll
@@ -879,7 +933,7 @@ void launch_shared(const FewArgs &a, hipStream_t s) {
                      dim3(kSharedWaves * 64), 0, s, a);
 }
 
-// Which kernel takes a call.  Times in us, kernels alone, d_model 2048, d_ff 4096, 8 experts, top-1 unless another size stands there.
+// Which kernel takes a call.  Times in us, kernels alone (side by side, 0.5 to 1 longer than now: find_piece for every size), d_model 2048, d_ff 4096, 8 experts, top-1 unless another size stands there.
 //  one token             one_token_kernel, but for gate | up in 4 bits (6.3 against 7.2) and 4-bit projections of 4096 rows and
 //                        more (8192 x 2048: 5.4 against 7.2), which have row tiles enough for the other kernel
 //  many slots an expert  shared_slots_kernel where the weights are no longer most of what comes into a CU.  Gate | up, 4 bits:
