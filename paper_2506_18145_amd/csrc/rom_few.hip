@@ -539,8 +539,8 @@ __device__ __forceinline__ int nth_bit(unsigned long long mask, int n) {
 }
 
 // The same for up to 64 slots, a lane each, without LDS and barriers: every wavefront by itself, expert after expert in the order in
-// which the slots name them.  0.5 to 1 us of every launch (one token's gate | up in 4 bits 6.2 -> 5.7), 1.6 of 8 tokens top-2's down projection
-// (12.9 -> 11.3).  my_slot: of column lane % 16 (past the end: of the first column).
+// which the slots name them.  It takes 0.5 to 1 us off a launch (one token's gate | up in 4 bits 6.2 to 5.7), 1.6 off 8 tokens
+// top-2's down projection (12.9 to 11.2).  my_slot: of column lane % 16 (past the end: of the first column).
 template <typename T, bool SWIGLU, int ROWS>
 __device__ __forceinline__ bool find_piece_64(const FewArgs &a, int row0, int &e, int &n_cols, int &my_slot) {
   const int lane = threadIdx.x & 63, S = a.N * a.K;
@@ -933,7 +933,8 @@ void launch_shared(const FewArgs &a, hipStream_t s) {
                      dim3(kSharedWaves * 64), 0, s, a);
 }
 
-// Which kernel takes a call.  Times in us, kernels alone (side by side, 0.5 to 1 longer than now: find_piece for every size), d_model 2048, d_ff 4096, 8 experts, top-1 unless another size stands there.
+// Which kernel takes a call.  Times in us, kernels alone, d_model 2048, d_ff 4096, 8 experts, top-1 unless another size stands
+// there; both sides with find_piece, many_slots_kernel up to 64 slots thus 0.5 to 1 longer than with find_piece_64.
 //  one token             one_token_kernel, but for gate | up in 4 bits (6.3 against 7.2) and 4-bit projections of 4096 rows and
 //                        more (8192 x 2048: 5.4 against 7.2), which have row tiles enough for the other kernel
 //  many slots an expert  shared_slots_kernel where the weights are no longer most of what comes into a CU.  Gate | up, 4 bits:
