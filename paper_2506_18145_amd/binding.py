@@ -608,7 +608,7 @@ def _keep_if_captured(kept: list, *buffers) -> None:
 
 
 def _not_while_capturing(what: str) -> None:
-    """What a holder lays out once would, under capture, be laid out by the graph's replays only."""
+    """What a holder lays out once would, under capture, be laid out by the graph's replays only, and by every one of them."""
     if torch.cuda.is_current_stream_capturing():
         raise RomError(f"{what} has to be called once before a capture: it packs the weights")
 
@@ -1148,8 +1148,11 @@ class RomFfnMoe:
     def step(self, x: torch.Tensor, expert_idx: torch.Tensor, gate: torch.Tensor, pre_norm: bool = False, add_skip: bool = False,
              q4_group: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """The layer on up to ROM_FEW_TOKENS tokens x [N, d_model], straight from the routing decision expert_idx, gate
-        [N, K] (rom_ffn_moe_step); q4_group 32, 64 or 128: with the weights in 4 bits."""
+        [N, K] (rom_ffn_moe_step); q4_group 32, 64 or 128: with the weights in 4 bits.  The first call of a pre_norm and
+        a q4_group lays out the weights: it has to come before a capture."""
         n, d = x.shape[0], self.dims
+        if not q4_group and bool(pre_norm) not in self._packed:
+            _not_while_capturing("RomFfnMoe.step")
         out = torch.empty_like(x) if out is None else out
         if self._step_ws is None:             # for ROM_FEW_TOKENS tokens: never replaced
             need = rom_ffn_step_workspace_bytes(d, self.d_ff, ROM_FEW_TOKENS)
@@ -1166,6 +1169,8 @@ class RomFfnMoe:
         if pre_norm not in self._packed:
             out = torch.empty_like(self.w_gate_up)
             rom_ffn_pack_gate_up(self.dims, self.d_ff, self.w_gate_up, self.norm_w if pre_norm else None, out)
+            if torch.cuda.is_current_stream_capturing():
+                return out                    # written by the graph's replays alone: not what an eager call may read
             self._packed[pre_norm] = out
             if drop_plain:
                 torch.cuda.synchronize()

@@ -1,0 +1,86 @@
+"""The holders of the few-token calls without a GPU: which buffers outlive a captured call, which weights and workspaces are
+refused.  Tensors lie on the CPU; the library's size functions are real, the calls that launch are recorded."""
+import gc
+import weakref
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+from paper_2506_18145_amd import binding
+from paper_2506_18145_amd.build import build_library
+
+E, D, DE, F = 4, 64, 128, 32
+
+
+class Recorder:
+    """The library with its launching calls replaced by ones that succeed and are counted."""
+
+    def __init__(self, lib):
+        self.lib, self.calls = lib, []
+
+    def __getattr__(self, name):
+        if name.endswith(("_bytes", "_layout")):
+            return getattr(self.lib, name)
+
+        def call(*args):
+            self.calls.append(name)
+            return 0
+        return call
+
+
+@pytest.fixture
+def host(monkeypatch):
+    import os
+    if not os.path.exists(binding._LIB_PATH):
+        build_library()
+    h = SimpleNamespace(lib=Recorder(binding.load_library()), capturing=False)
+    monkeypatch.setattr(binding, "load_library", lambda: h.lib)
+    monkeypatch.setattr(binding, "_current_index", lambda t: t.get_device())
+    monkeypatch.setattr(binding, "_raw_stream", lambda index: 0)
+    monkeypatch.setattr(binding, "_stream", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: h.capturing)
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    return h
+
+
+def layer_of(top_k=1, dtype="bf16"):
+    cfg = SimpleNamespace(d_model=D, d_inner=DE, d_state=16, d_conv=4, dt_rank=8, n_experts=E, top_k=top_k, n_experts_xdt=E,
+                          dtype=dtype, gate_mode=1 if top_k > 1 else 0)
+    zeros = torch.zeros
+    return binding.RomLayer(cfg, dict(
+        w_router=zeros(E, D), b_router=None, w_in=zeros(E, 2 * DE, D), conv_w=zeros(DE, 4), conv_b=zeros(DE), w_x=zeros(E, 40, DE),
+        w_dt=zeros(E, DE, 8), dt_bias=zeros(DE), A_log=zeros(DE, 16), D=zeros(DE), w_out=zeros(E, D, DE), norm_w=torch.ones(D)), device="cpu")
+
+
+def ffn_of(layer):
+    return binding.RomFfnMoe(layer, F, dict(w_gate_up=torch.zeros(E, 2 * F, D), w_down=torch.zeros(E, D, F), norm_w=torch.ones(D)))
+
+
+def tokens(n, k=1, dtype=torch.bfloat16):
+    return torch.zeros(n, D, dtype=dtype), torch.zeros(n, k, dtype=torch.int32), torch.ones(n, k)
+
+
+# ---------------------------------------------------------------- captures
+
+
+def test_a_captured_packing_is_not_what_an_eager_call_takes(host):
+    """Under capture the packing of gate | up is only recorded: its result is the graph's, and a step asks for an eager call first."""
+    ffn = ffn_of(layer_of())
+    x, idx, gate = tokens(3)
+    routing = dict.fromkeys(("offsets", "perm", "inv_perm"), idx) | {"gate": gate}
+    host.capturing = True
+    for pre_norm in (False, True):
+        with pytest.raises(binding.RomError, match="before a capture"):
+            ffn.step(x, idx, gate, pre_norm)
+        ffn.forward(x, routing, pre_norm)                       # lays out its weights in front of its products, in every replay
+    assert host.lib.calls == ["rom_ffn_pack_gate_up", "rom_ffn_moe_forward"] * 2
+    host.capturing = False
+    host.lib.calls.clear()
+    ffn.step(x, idx, gate, True)
+    ffn.forward(x, routing, True)
+    assert host.lib.calls == ["rom_ffn_pack_gate_up", "rom_ffn_moe_step", "rom_ffn_moe_forward"]
+    host.capturing = True
+    ffn.step(x, idx, gate, True)
+    with pytest.raises(binding.RomError, match="before a capture"):
+        ffn.step(x, idx, gate, False)                           # packed without the norm's scale: another layout

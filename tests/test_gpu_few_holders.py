@@ -1,0 +1,36 @@
+"""The holders of the few-token calls on the GPU: captures beside eager calls of the same holder."""
+import pytest
+import torch
+
+from paper_2506_18145_amd import RomError
+from tests.test_gpu_few_tokens import ffn_holder, randn, routing
+
+pytestmark = pytest.mark.gpu
+
+
+def test_a_forward_captured_first_leaves_eager_calls_their_weights():
+    """Fresh holder, one for each pre_norm: the capture's packing has not run when the eager calls in front of a replay read theirs."""
+    for pre_norm in (False, True):
+        cfg, layer, ffn = ffn_holder(64, 32, 4, 1, "bf16")
+        _, _, other = ffn_holder(64, 32, 4, 1, "bf16")
+        x = randn(1, 3, 64)
+        r = layer.route(x)
+        want = other.forward(x, r, pre_norm), other.step(x, r["expert_idx"], r["gate"], pre_norm)
+        ffn._ws, ffn._step_ws = (torch.empty_like(w) for w in (other._ws, other._step_ws))
+        out, refused = torch.empty_like(x), False
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            ffn.forward(x, r, pre_norm, out=out)
+            try:
+                ffn.step(x, r["expert_idx"], r["gate"], pre_norm)
+            except RomError as e:
+                refused = "before a capture" in str(e)
+        assert refused
+        assert torch.equal(ffn.step(x, r["expert_idx"], r["gate"], pre_norm), want[1]) and torch.equal(ffn.forward(x, r, pre_norm), want[0])
+        for _ in range(3):
+            out.fill_(float("nan"))
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want[0])
+            assert torch.equal(ffn.step(x, r["expert_idx"], r["gate"], pre_norm), want[1])
