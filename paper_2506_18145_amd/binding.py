@@ -1298,9 +1298,10 @@ class RomHybridStack:
             n, d = len(self.layers), self.dims
             conv_out = torch.empty((n, B, d.d_inner, d.d_conv - 1), dtype=torch.float32, device=self.device)
             ssm_out = torch.empty((n, B, d.d_inner, d.d_state), dtype=torch.float32, device=self.device)
+        ws = self.layers[0].workspace(max(B, 1), max(L, 1))
+        _keep_if_captured(self._kept, self._tmp, self._ffn_ws, ws)
         rom_hybrid_stack_forward(self.dims, self.d_ff, self.blocks, self.ffn_structs, self.ffn_pre_norm, self.eps, x,
-                                 B, L, conv_state, ssm_state, out, conv_out, ssm_out, self._tmp,
-                                 self.layers[0].workspace(max(B, 1), max(L, 1)), self._ffn_ws)
+                                 B, L, conv_state, ssm_state, out, conv_out, ssm_out, self._tmp, ws, self._ffn_ws)
         return (out, conv_out, ssm_out) if return_states else out
 
     def quantize(self, group: int = 64) -> "RomHybridStack":

@@ -84,3 +84,28 @@ def test_a_captured_packing_is_not_what_an_eager_call_takes(host):
     ffn.step(x, idx, gate, True)
     with pytest.raises(binding.RomError, match="before a capture"):
         ffn.step(x, idx, gate, False)                           # packed without the norm's scale: another layout
+
+
+def hybrid_of(n_layers=2):
+    layers = [layer_of() for _ in range(n_layers)]
+    return binding.RomHybridStack(layers, [ffn_of(ly) for ly in layers])
+
+
+def states(B, n_layers=None):
+    lead = () if n_layers is None else (n_layers,)
+    return torch.zeros(*lead, B, DE, 3), torch.zeros(*lead, B, DE, 16)
+
+
+def let_go(*buffers):
+    gc.collect()
+    return [r() is None for r in buffers]
+
+
+def test_a_captured_stack_forward_keeps_its_buffers(host):
+    stack = hybrid_of()
+    host.capturing = True
+    stack.forward(torch.zeros(2, 3, D, dtype=torch.bfloat16))
+    host.capturing = False
+    used = [weakref.ref(b) for b in (stack._tmp, stack._ffn_ws)]
+    stack.step(torch.zeros(40, D, dtype=torch.bfloat16), *states(40, 2))       # another shape, more tokens
+    assert let_go(*used) == [False, False]

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2506_18145_amd import RomError
-from tests.test_gpu_few_tokens import ffn_holder, randn, routing
+from tests.test_gpu_few_tokens import ffn_holder, hybrid, randn, routing, states, step_cfg
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +34,25 @@ def test_a_forward_captured_first_leaves_eager_calls_their_weights():
             torch.cuda.synchronize()
             assert torch.equal(out, want[0])
             assert torch.equal(ffn.step(x, r["expert_idx"], r["gate"], pre_norm), want[1])
+
+
+@pytest.mark.parametrize("K", [1, 2])
+def test_a_captured_stack_forward_replayed_behind_steps(K):
+    cfg = step_cfg(batch=2, top_k=K, gate_mode=K - 1)
+    stack = hybrid(cfg)
+    x = randn(1, 2, 5, cfg.d_model)
+    want = stack.forward(x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = stack.forward(x)
+    for t in range(3):
+        big = step_cfg(batch=60 + 30 * t, top_k=K, gate_mode=K - 1)     # other shapes, larger workspaces
+        for group in (0, 64):
+            stack.step(randn(t, big.batch, cfg.d_model), *states(big, 7, 3), q4_group=group)
+        fill = [torch.full((1 << 20,), -1, dtype=torch.int32, device=x.device) for _ in range(8)]     # takes what was let go
+        got.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and all(bool((f == -1).all()) for f in fill)
+        del fill
