@@ -911,6 +911,7 @@ class RomLayer:
             raise RomError("rom_workspace_bytes returned 0: unsupported dims")
         if self._ws is None or self._ws.numel() < need:
             self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        _keep_if_captured(self._kept, self._ws)
         return self._ws
 
     def ws_view(self, name: str, B: int, L: int) -> torch.Tensor:

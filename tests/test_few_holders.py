@@ -41,6 +41,8 @@ def host(monkeypatch):
     monkeypatch.setattr(binding, "_stream", lambda: 0)
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: h.capturing)
     monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    monkeypatch.setattr(binding.RomQ4Weight, "pack", lambda w, group=64: SimpleNamespace(
+        packed=torch.zeros(binding.rom_q4_bytes(*w.shape, group), dtype=torch.uint8)))
     return h
 
 
@@ -109,3 +111,19 @@ def test_a_captured_stack_forward_keeps_its_buffers(host):
     used = [weakref.ref(b) for b in (stack._tmp, stack._ffn_ws)]
     stack.step(torch.zeros(40, D, dtype=torch.bfloat16), *states(40, 2))       # another shape, more tokens
     assert let_go(*used) == [False, False]
+
+
+def test_a_captured_plain_step_keeps_its_workspace(host):
+    layer = layer_of(top_k=2)
+    x = torch.zeros(4, D, dtype=torch.bfloat16)
+    for call in (layer.step, layer.block_step):
+        layer._ws = None
+        host.capturing = True
+        call(x, *states(4))
+        host.capturing = False
+        used = weakref.ref(layer._ws)
+        layer.step_q4(x, *states(4))                            # the same batch needs more with 4-bit projections
+        assert layer._ws is not used() and let_go(used) == [False]
+        used = weakref.ref(layer._ws)
+        layer.forward(torch.zeros(4, 500, D, dtype=torch.bfloat16))
+        assert let_go(used) == [True]                           # no capture: nothing piles up

@@ -56,3 +56,28 @@ def test_a_captured_stack_forward_replayed_behind_steps(K):
         torch.cuda.synchronize()
         assert torch.equal(got, want) and all(bool((f == -1).all()) for f in fill)
         del fill
+
+
+@pytest.mark.parametrize("block", [False, True])
+def test_a_captured_plain_step_replayed_behind_4_bit_steps(block):
+    cfg, layer, _ = ffn_holder(128, 256, 8, 2, "bf16")
+    layer.weights["norm_w"] = torch.ones(128, device="cuda:0")
+    step = layer.block_step if block else layer.step
+    x = randn(1, 5, 128)
+    cs0, ss0 = randn(2, 5, 256, 3, dtype="fp32"), randn(3, 5, 256, 16, dtype="fp32")
+    cs, ss = cs0.clone(), ss0.clone()
+    want = step(x, cs, ss)                                      # folds the norm's scale, makes the workspace
+    want_cs, want_ss = cs.clone(), ss.clone()
+    out = torch.empty_like(x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(x, cs, ss, out)
+    for _ in range(3):
+        (layer.block_step_q4 if block else layer.step_q4)(x, cs0.clone(), ss0.clone())       # the same batch, a larger workspace
+        fill = [torch.full((n,), -1, dtype=torch.int32, device=x.device) for n in (1 << 12, 1 << 14, 1 << 16, 1 << 18)]
+        cs.copy_(cs0), ss.copy_(ss0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(cs, want_cs) and torch.equal(ss, want_ss)
+        assert all(bool((f == -1).all()) for f in fill)
