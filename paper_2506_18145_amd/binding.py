@@ -637,9 +637,11 @@ def _weight_bytes(n_mats: int, rows: int, cols: int, group: int, element_size: i
     return codes + 4 * codes // group
 
 
-def _expect_weight(t: torch.Tensor, what: str, need: int, index: int) -> None:
-    if t.numel() * t.element_size() != need or t.get_device() != index or not t.is_contiguous():
-        raise RomError(f"{what}: expected {need} contiguous bytes on cuda:{index}, got {t.numel() * t.element_size()} on {t.device}")
+def _expect_weight(t: torch.Tensor, what: str, dtype, need: int, index: int) -> None:
+    """dtype: the activations' for a plain stack, uint8 for one in 4 bits."""
+    if t.dtype is not dtype or t.numel() * t.element_size() != need or t.get_device() != index or not t.is_contiguous():
+        raise RomError(f"{what}: expected {need} contiguous bytes of {dtype} on cuda:{index}, got {t.numel() * t.element_size()} of "
+                       f"{t.dtype} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
 
 
 def rom_q4_pack(w: torch.Tensor, group: int, w_q4: torch.Tensor) -> None:
@@ -669,7 +671,7 @@ def rom_q4_project_workspace_bytes(rows: int, top_k: int, n_tokens: int) -> int:
 def rom_q4_project(w_q4, n_mats, rows, cols, group, x, expert_idx, gate, row_scale, residual, out, ws):
     """x [N, cols], out [N, rows]; top_k is expert_idx's second size (1 without)."""
     if group > 0:                                   # else the library refuses it
-        _expect_weight(w_q4, "w_q4", _weight_bytes(n_mats, rows, cols, group, 1), x.get_device())
+        _expect_weight(w_q4, "w_q4", torch.uint8, _weight_bytes(n_mats, rows, cols, group, 1), x.get_device())
     _q4_project(w_q4, n_mats, rows, cols, group, x, 1 if expert_idx is None else expert_idx.shape[-1], expert_idx, gate, row_scale,
                 residual, out, ws)
 
@@ -703,9 +705,9 @@ def rom_ffn_moe_step(dims, d_ff, w_gate_up, w_down, q4_group, pre_norm, eps, add
     _expect(out, "out", dtype, (n_tokens, dims.d_model), index)
     _expect(expert_idx, "expert_idx", torch.int32, (n_tokens, k), index)
     _expect(gate, "gate", torch.float32, (n_tokens, k), index)
-    size = x.element_size()
-    _expect_weight(w_gate_up, "w_gate_up", _weight_bytes(dims.n_experts, 2 * d_ff, dims.d_model, q4_group, size), index)
-    _expect_weight(w_down, "w_down", _weight_bytes(dims.n_experts, dims.d_model, d_ff, q4_group, size), index)
+    size, held = x.element_size(), torch.uint8 if q4_group else dtype
+    _expect_weight(w_gate_up, "w_gate_up", held, _weight_bytes(dims.n_experts, 2 * d_ff, dims.d_model, q4_group, size), index)
+    _expect_weight(w_down, "w_down", held, _weight_bytes(dims.n_experts, dims.d_model, d_ff, q4_group, size), index)
     w = _RomFfnWeights(w_gate_up.data_ptr(), w_down.data_ptr())
     code = load_library().rom_ffn_moe_step(
         ctypes.byref(dims), d_ff, ctypes.byref(w), q4_group, 1 if pre_norm else 0, eps, 1 if add_skip else 0, x.data_ptr(),

@@ -127,3 +127,38 @@ def test_a_captured_plain_step_keeps_its_workspace(host):
         used = weakref.ref(layer._ws)
         layer.forward(torch.zeros(4, 500, D, dtype=torch.bfloat16))
         assert let_go(used) == [True]                           # no capture: nothing piles up
+
+
+# ---------------------------------------------------------------- what is refused
+
+
+def raw_ffn_step(dims, gu, down, group=0, dtype=torch.bfloat16, n=3, ws=None):
+    x, idx, gate = tokens(n, dims.top_k, dtype)
+    ws = torch.zeros(binding.rom_ffn_step_workspace_bytes(dims, F, n), dtype=torch.uint8) if ws is None else ws
+    binding.rom_ffn_moe_step(dims, F, gu, down, group, False, 1e-5, False, x, n, idx, gate, torch.empty_like(x), ws)
+
+
+def packed_of(rows, cols, group=32):
+    return torch.zeros(binding.rom_q4_bytes(E, rows, cols, group), dtype=torch.uint8)
+
+
+def test_weights_of_another_type_of_the_same_size(host):
+    for tdtype, others in ((torch.bfloat16, (torch.float16, torch.int16)), (torch.float32, (torch.int32,))):
+        dims = layer_of(dtype="bf16" if tdtype is torch.bfloat16 else "fp32").dims
+        gu, down = torch.zeros(E, 2 * F, D, dtype=tdtype), torch.zeros(E, D, F, dtype=tdtype)
+        raw_ffn_step(dims, gu, down, dtype=tdtype)
+        for other in others:
+            for w in ((gu.view(other), down), (gu, down.view(other))):
+                with pytest.raises(binding.RomError):
+                    raw_ffn_step(dims, *w, dtype=tdtype)
+        gu, down = packed_of(2 * F, D), packed_of(D, F)
+        raw_ffn_step(dims, gu, down, 32, tdtype)
+        for w in ((gu.view(tdtype), down), (gu, down.view(torch.int8))):
+            with pytest.raises(binding.RomError):
+                raw_ffn_step(dims, *w, 32, tdtype)
+    q, x = packed_of(64, D), tokens(3)[0]
+    out, idx = torch.zeros(3, 64, dtype=x.dtype), torch.zeros(3, 1, dtype=torch.int32)
+    binding.rom_q4_project(q, E, 64, D, 32, x, idx, None, None, None, out, None)
+    with pytest.raises(binding.RomError):
+        binding.rom_q4_project(q.view(torch.bfloat16), E, 64, D, 32, x, idx, None, None, None, out, None)
+    assert host.lib.calls == ["rom_ffn_moe_step"] * 4 + ["rom_q4_project"]
