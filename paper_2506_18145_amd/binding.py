@@ -394,12 +394,29 @@ def rom_block_step(dims, weights, norm_weight, eps, x, B, conv_state, ssm_state,
     _check(code, "rom_block_step")
 
 
+def _kinds(first, second) -> tuple:
+    """What two weight tensors are, beside their addresses: type, bytes, device."""
+    return tuple((t.dtype, t.numel() * t.element_size(), t.get_device()) for t in (first, second) if t is not None)
+
+
 def make_blocks(layers):
-    """Host array of rom_block for a list of (weights dict with folded w_in, norm_weight) pairs."""
+    """Host array of rom_block for a list of (weights dict with folded w_in, norm_weight) pairs.  Its attribute kinds says
+    what the blocks' projections are: a call that reads them as something else would read past their ends."""
     arr = (_RomBlock * len(layers))()
     for j, (w, norm_weight) in enumerate(layers):
         arr[j].w = _weights_struct(w)
         arr[j].norm_weight = _ptr(norm_weight)
+    arr.kinds = {_kinds(w.get("w_in"), w.get("w_out")) for w, _ in layers}
+    return arr
+
+
+def make_ffns(layers):
+    """Host array of rom_ffn_weights for a list of (w_gate_up packed, w_down) pairs or None; kinds as make_blocks."""
+    arr = (_RomFfnWeights * len(layers))()
+    for j, w in enumerate(layers):
+        if w is not None:
+            arr[j] = _RomFfnWeights(_ptr(w[0]), _ptr(w[1]))
+    arr.kinds = {_kinds(*w) for w in layers if w is not None}
     return arr
 
 
@@ -637,8 +654,10 @@ def _weight_bytes(n_mats: int, rows: int, cols: int, group: int, element_size: i
     return codes + 4 * codes // group
 
 
-def _expect_weight(t: torch.Tensor, what: str, dtype, need: int, index: int) -> None:
+def _expect_weight(t: Optional[torch.Tensor], what: str, dtype, need: int, index: int) -> None:
     """dtype: the activations' for a plain stack, uint8 for one in 4 bits."""
+    if t is None:
+        raise RomError(f"{what} is missing")
     if t.dtype is not dtype or t.numel() * t.element_size() != need or t.get_device() != index or not t.is_contiguous():
         raise RomError(f"{what}: expected {need} contiguous bytes of {dtype} on cuda:{index}, got {t.numel() * t.element_size()} of "
                        f"{t.dtype} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
@@ -720,7 +739,15 @@ def rom_step_q4_workspace_bytes(dims, B: int) -> int:
     return int(load_library().rom_step_q4_workspace_bytes(ctypes.byref(dims), B))
 
 
+def _expect_projections(dims, weights, q4_group: int, index: int) -> None:
+    if q4_group > 0:                                # else the library refuses it
+        E, De, D = dims.n_experts, dims.d_inner, dims.d_model
+        _expect_weight(weights.get("w_in"), "w_in", torch.uint8, _weight_bytes(E, 2 * De, D, q4_group, 1), index)
+        _expect_weight(weights.get("w_out"), "w_out", torch.uint8, _weight_bytes(E, D, De, q4_group, 1), index)
+
+
 def rom_step_q4(dims, weights, q4_group, x, B, conv_state, ssm_state, out, ws):
+    _expect_projections(dims, weights, q4_group, _current_index(x))
     code = load_library().rom_step_q4(
         ctypes.byref(dims), ctypes.byref(_weights_struct(weights)), q4_group, _ptr(x), B, _ptr(conv_state), _ptr(ssm_state),
         _ptr(out), _ptr(ws), _nbytes(ws), _stream())
@@ -728,6 +755,7 @@ def rom_step_q4(dims, weights, q4_group, x, B, conv_state, ssm_state, out, ws):
 
 
 def rom_block_step_q4(dims, weights, q4_group, norm_weight, eps, x, B, conv_state, ssm_state, out, ws):
+    _expect_projections(dims, weights, q4_group, _current_index(x))
     code = load_library().rom_block_step_q4(
         ctypes.byref(dims), ctypes.byref(_weights_struct(weights)), q4_group, _ptr(norm_weight), eps, _ptr(x), B,
         _ptr(conv_state), _ptr(ssm_state), _ptr(out), _ptr(ws), _nbytes(ws), _stream())
@@ -738,8 +766,23 @@ def rom_hybrid_step_ffn_workspace_bytes(dims, d_ff: int, B: int, q4_group: int) 
     return int(load_library().rom_hybrid_step_ffn_workspace_bytes(ctypes.byref(dims), d_ff, B, q4_group))
 
 
+@functools.lru_cache(maxsize=None)
+def _stack_kinds(n_experts: int, d_inner: int, d_model: int, d_ff: int, q4_group: int, dtype, index: int) -> tuple:
+    """_kinds of a block's projections and of an FFN-MoE layer's weights in a stack of these sizes."""
+    t, size = (torch.uint8, 1) if q4_group else (dtype, dtype.itemsize)
+    return tuple(tuple((t, _weight_bytes(n_experts, rows, cols, q4_group, size), index) for rows, cols in shapes)
+                 for shapes in (((2 * d_inner, d_model), (d_model, d_inner)), ((2 * d_ff, d_model), (d_model, d_ff))))
+
+
 def rom_hybrid_stack_step(dims, d_ff, blocks, ffns, q4_group, ffn_pre_norm, eps, x, B, conv_state, ssm_state, out, tmp, ws,
                           ffn_ws):
+    """blocks, ffns: make_blocks, make_ffns (arrays put together otherwise are taken as they are)."""
+    index, dtype = _current_index(x), _TORCH_TYPE.get(dims.dtype)
+    if q4_group >= 0 and dtype is not None:         # else the library refuses it
+        for arr, what, want in zip((blocks, ffns), ("blocks", "ffns"),
+                                   _stack_kinds(dims.n_experts, dims.d_inner, dims.d_model, d_ff, q4_group, dtype, index)):
+            if getattr(arr, "kinds", set()) - {want}:
+                raise RomError(f"{what}: expected weights of (type, bytes, device) {want} for q4_group {q4_group}, got {arr.kinds}")
     code = load_library().rom_hybrid_stack_step(
         ctypes.byref(dims), d_ff, blocks, ffns, q4_group, int(bool(ffn_pre_norm)), len(blocks), eps, _ptr(x), B,
         _ptr(conv_state), _ptr(ssm_state), _ptr(out), _ptr(tmp), _ptr(ws), _nbytes(ws), _ptr(ffn_ws), _nbytes(ffn_ws),
@@ -1279,10 +1322,7 @@ class RomHybridStack:
         self._keep = [(ly.block_weights(in_place=fold_in_place), ly.weights["norm_w"]) for ly in self.layers]
         self.blocks = make_blocks(self._keep)
         self._packed = [None if f is None else f.packed(ffn_pre_norm) for f in self.ffns]
-        self.ffn_structs = (_RomFfnWeights * len(self.ffns))()
-        for j, f in enumerate(self.ffns):
-            if f is not None:
-                self.ffn_structs[j] = _RomFfnWeights(_ptr(self._packed[j]), _ptr(f.w_down))
+        self.ffn_structs = make_ffns([None if f is None else (w, f.w_down) for f, w in zip(self.ffns, self._packed)])
         self._tmp: Optional[torch.Tensor] = None
         self._ffn_ws: Optional[torch.Tensor] = None
         self._q4: Dict[int, tuple] = {}
@@ -1311,12 +1351,8 @@ class RomHybridStack:
         """Packs the projections and FFN weights of every layer in 4 bits for step(..., q4_group=group)."""
         if group not in self._q4:
             keep = [(ly.q4_weights(group, block=True), ly.weights["norm_w"]) for ly in self.layers]
-            structs = (_RomFfnWeights * len(self.ffns))()
             ffn_keep = [None if f is None else f.q4_weights(group, self.ffn_pre_norm) for f in self.ffns]
-            for j, w in enumerate(ffn_keep):
-                if w is not None:
-                    structs[j] = _RomFfnWeights(_ptr(w[0]), _ptr(w[1]))
-            self._q4[group] = (make_blocks(keep), structs, keep, ffn_keep)
+            self._q4[group] = (make_blocks(keep), make_ffns(ffn_keep), keep, ffn_keep)
         return self
 
     def state_shapes(self, B: int):

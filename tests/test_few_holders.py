@@ -162,3 +162,54 @@ def test_weights_of_another_type_of_the_same_size(host):
     with pytest.raises(binding.RomError):
         binding.rom_q4_project(q.view(torch.bfloat16), E, 64, D, 32, x, idx, None, None, None, out, None)
     assert host.lib.calls == ["rom_ffn_moe_step"] * 4 + ["rom_q4_project"]
+
+
+def raw_steps(layer, group, weights, B=3):
+    """The step and the block step as the C ABI's wrappers take them."""
+    x, out, ws = tokens(B, dtype=layer.tdtype)[0], tokens(B, dtype=layer.tdtype)[0], torch.zeros(binding.rom_step_q4_workspace_bytes(layer.dims, B), dtype=torch.uint8)
+    cs, ss = states(B)
+    return (lambda **kw: binding.rom_step_q4(**dict(dict(dims=layer.dims, weights=weights, q4_group=group, x=x, B=B, conv_state=cs, ssm_state=ss,
+                                                         out=out, ws=ws), **kw)),
+            lambda **kw: binding.rom_block_step_q4(**dict(dict(dims=layer.dims, weights=weights, q4_group=group, norm_weight=layer.weights["norm_w"],
+                                                               eps=1e-5, x=x, B=B, conv_state=cs, ssm_state=ss, out=out, ws=ws), **kw)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_steps_refuse_weights_of_another_group_or_layer(host, dtype):
+    """Scales of 128 columns read as those of 32 would be read four times past their end."""
+    layer = layer_of(dtype=dtype)
+    for held, told in ((128, 32), (32, 128), (64, 32)):
+        for call in raw_steps(layer, told, layer.q4_weights(held)):
+            with pytest.raises(binding.RomError):
+                call()
+            call(weights=layer.q4_weights(told))
+            for name in ("w_in", "w_out"):
+                for bad in (layer.weights[name], layer.q4_weights(told)[name][:-2], None):
+                    with pytest.raises(binding.RomError):
+                        call(weights=dict(layer.q4_weights(told), **{name: bad}))
+    assert host.lib.calls == ["rom_step_q4", "rom_block_step_q4"] * 3
+
+
+def test_stack_step_refuses_weights_of_another_group(host):
+    stack = hybrid_of(3)
+    stack.quantize(32).quantize(128)
+    B = 3
+    x, (cs, ss) = tokens(B)[0], states(B, 3)
+    ws, ffn_ws = torch.zeros(1 << 20, dtype=torch.uint8), torch.zeros(1 << 20, dtype=torch.uint8)
+
+    def call(blocks, ffns, group):
+        binding.rom_hybrid_stack_step(stack.dims, F, blocks, ffns, group, True, 1e-5, x, B, cs, ss, x.clone(), x.clone(), ws, ffn_ws)
+
+    held = {0: (stack.blocks, stack.ffn_structs), 32: stack._q4[32][:2], 128: stack._q4[128][:2]}
+    for told in held:
+        call(*held[told], told)
+        for other in held:
+            if other != told:
+                for blocks, ffns in ((held[other][0], held[told][1]), (held[told][0], held[other][1])):
+                    with pytest.raises(binding.RomError):
+                        call(blocks, ffns, told)
+    with pytest.raises(binding.RomError):                       # one block of three
+        keep = [(ly.q4_weights(32, block=True), ly.weights["norm_w"]) for ly in stack.layers]
+        keep[2] = stack.layers[2].q4_weights(128, block=True), keep[2][1]
+        call(binding.make_blocks(keep), held[32][1], 32)
+    assert host.lib.calls.count("rom_hybrid_stack_step") == 3
