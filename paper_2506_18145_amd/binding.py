@@ -663,6 +663,12 @@ def _expect_weight(t: Optional[torch.Tensor], what: str, dtype, need: int, index
                        f"{t.dtype} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
 
 
+def _expect_ws(ws: Optional[torch.Tensor], index: int, what: str = "ws") -> None:
+    """The library sees a workspace's address and size; it refuses a missing one where it needs one."""
+    if ws is not None and (ws.get_device() != index or not ws.is_contiguous()):
+        raise RomError(f"{what}: expected contiguous memory on cuda:{index}, got {ws.device}{'' if ws.is_contiguous() else ', not contiguous'}")
+
+
 def rom_q4_pack(w: torch.Tensor, group: int, w_q4: torch.Tensor) -> None:
     """w [n_mats, rows, cols] -> w_q4 uint8 [rom_q4_bytes(...)]"""
     n, rows, cols = w.shape
@@ -691,6 +697,7 @@ def rom_q4_project(w_q4, n_mats, rows, cols, group, x, expert_idx, gate, row_sca
     """x [N, cols], out [N, rows]; top_k is expert_idx's second size (1 without)."""
     if group > 0:                                   # else the library refuses it
         _expect_weight(w_q4, "w_q4", torch.uint8, _weight_bytes(n_mats, rows, cols, group, 1), x.get_device())
+    _expect_ws(ws, x.get_device())
     _q4_project(w_q4, n_mats, rows, cols, group, x, 1 if expert_idx is None else expert_idx.shape[-1], expert_idx, gate, row_scale,
                 residual, out, ws)
 
@@ -727,10 +734,11 @@ def rom_ffn_moe_step(dims, d_ff, w_gate_up, w_down, q4_group, pre_norm, eps, add
     size, held = x.element_size(), torch.uint8 if q4_group else dtype
     _expect_weight(w_gate_up, "w_gate_up", held, _weight_bytes(dims.n_experts, 2 * d_ff, dims.d_model, q4_group, size), index)
     _expect_weight(w_down, "w_down", held, _weight_bytes(dims.n_experts, dims.d_model, d_ff, q4_group, size), index)
+    _expect_ws(ws, index)
     w = _RomFfnWeights(w_gate_up.data_ptr(), w_down.data_ptr())
     code = load_library().rom_ffn_moe_step(
         ctypes.byref(dims), d_ff, ctypes.byref(w), q4_group, 1 if pre_norm else 0, eps, 1 if add_skip else 0, x.data_ptr(),
-        n_tokens, expert_idx.data_ptr(), gate.data_ptr(), out.data_ptr(), ws.data_ptr(), _nbytes(ws), _raw_stream(index))
+        n_tokens, expert_idx.data_ptr(), gate.data_ptr(), out.data_ptr(), _at(ws), _nbytes(ws), _raw_stream(index))
     if code:
         _check(code, "rom_ffn_moe_step")
 
@@ -747,7 +755,9 @@ def _expect_projections(dims, weights, q4_group: int, index: int) -> None:
 
 
 def rom_step_q4(dims, weights, q4_group, x, B, conv_state, ssm_state, out, ws):
-    _expect_projections(dims, weights, q4_group, _current_index(x))
+    index = _current_index(x)
+    _expect_projections(dims, weights, q4_group, index)
+    _expect_ws(ws, index)
     code = load_library().rom_step_q4(
         ctypes.byref(dims), ctypes.byref(_weights_struct(weights)), q4_group, _ptr(x), B, _ptr(conv_state), _ptr(ssm_state),
         _ptr(out), _ptr(ws), _nbytes(ws), _stream())
@@ -755,7 +765,9 @@ def rom_step_q4(dims, weights, q4_group, x, B, conv_state, ssm_state, out, ws):
 
 
 def rom_block_step_q4(dims, weights, q4_group, norm_weight, eps, x, B, conv_state, ssm_state, out, ws):
-    _expect_projections(dims, weights, q4_group, _current_index(x))
+    index = _current_index(x)
+    _expect_projections(dims, weights, q4_group, index)
+    _expect_ws(ws, index)
     code = load_library().rom_block_step_q4(
         ctypes.byref(dims), ctypes.byref(_weights_struct(weights)), q4_group, _ptr(norm_weight), eps, _ptr(x), B,
         _ptr(conv_state), _ptr(ssm_state), _ptr(out), _ptr(ws), _nbytes(ws), _stream())
@@ -783,6 +795,8 @@ def rom_hybrid_stack_step(dims, d_ff, blocks, ffns, q4_group, ffn_pre_norm, eps,
                                    _stack_kinds(dims.n_experts, dims.d_inner, dims.d_model, d_ff, q4_group, dtype, index)):
             if getattr(arr, "kinds", set()) - {want}:
                 raise RomError(f"{what}: expected weights of (type, bytes, device) {want} for q4_group {q4_group}, got {arr.kinds}")
+    _expect_ws(ws, index)
+    _expect_ws(ffn_ws, index, "ffn_ws")
     code = load_library().rom_hybrid_stack_step(
         ctypes.byref(dims), d_ff, blocks, ffns, q4_group, int(bool(ffn_pre_norm)), len(blocks), eps, _ptr(x), B,
         _ptr(conv_state), _ptr(ssm_state), _ptr(out), _ptr(tmp), _ptr(ws), _nbytes(ws), _ptr(ffn_ws), _nbytes(ffn_ws),

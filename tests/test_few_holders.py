@@ -213,3 +213,33 @@ def test_stack_step_refuses_weights_of_another_group(host):
         keep[2] = stack.layers[2].q4_weights(128, block=True), keep[2][1]
         call(binding.make_blocks(keep), held[32][1], 32)
     assert host.lib.calls.count("rom_hybrid_stack_step") == 3
+
+
+class Elsewhere(torch.Tensor):
+    """A tensor of another device than the call's."""
+
+    def get_device(self):
+        return 7
+
+
+def test_workspaces_elsewhere_or_with_gaps(host):
+    layer = layer_of(top_k=2)
+    x, idx, gate = tokens(3, 2)
+    gu, down = torch.zeros(E, 2 * F, D, dtype=x.dtype), torch.zeros(E, D, F, dtype=x.dtype)
+    q, out = packed_of(64, D), torch.zeros(3, 64, dtype=x.dtype)
+    stack = hybrid_of(2)
+    stack.quantize(32)
+    cs, ss = states(3, 2)
+    size = 1 << 20
+    calls = [lambda ws: raw_ffn_step(layer.dims, gu, down, ws=ws), lambda ws: binding.rom_q4_project(q, E, 64, D, 32, x, idx, gate, None, None, out, ws)]
+    calls += [lambda ws, c=c: c(ws=ws) for c in raw_steps(layer, 32, layer.q4_weights(32))]
+    for mine in (lambda ws: (ws, torch.zeros(size, dtype=torch.uint8)), lambda ws: (torch.zeros(size, dtype=torch.uint8), ws)):
+        calls.append(lambda ws, mine=mine: binding.rom_hybrid_stack_step(stack.dims, F, *stack._q4[32][:2], 32, True, 1e-5, x, 3, cs, ss, x.clone(),
+                                                                          x.clone(), *mine(ws)))
+    for call in calls:
+        call(torch.zeros(size, dtype=torch.uint8))
+        n = len(host.lib.calls)
+        for ws in (torch.zeros(size, dtype=torch.uint8).as_subclass(Elsewhere), torch.zeros(size, 2, dtype=torch.uint8)[:, 0]):
+            with pytest.raises(binding.RomError):
+                call(ws)
+        assert len(host.lib.calls) == n
