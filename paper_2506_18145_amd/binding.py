@@ -754,8 +754,18 @@ def _expect_projections(dims, weights, q4_group: int, index: int) -> None:
         _expect_weight(weights.get("w_out"), "w_out", torch.uint8, _weight_bytes(E, D, De, q4_group, 1), index)
 
 
+def _expect_step(dims, x, B: int, conv_state, ssm_state, out, lead: tuple = ()) -> int:
+    """One token of each of B sequences and the states of one layer (lead (): else of so many); x's device index."""
+    index, dtype = _current_index(x), _TORCH_TYPE.get(dims.dtype)
+    _expect(x, "x", dtype, (B, dims.d_model), index)
+    _expect(out, "out", dtype, (B, dims.d_model), index)
+    _expect(conv_state, "conv_state", torch.float32, (*lead, B, dims.d_inner, dims.d_conv - 1), index)
+    _expect(ssm_state, "ssm_state", torch.float32, (*lead, B, dims.d_inner, dims.d_state), index)
+    return index
+
+
 def rom_step_q4(dims, weights, q4_group, x, B, conv_state, ssm_state, out, ws):
-    index = _current_index(x)
+    index = _expect_step(dims, x, B, conv_state, ssm_state, out)
     _expect_projections(dims, weights, q4_group, index)
     _expect_ws(ws, index)
     code = load_library().rom_step_q4(
@@ -765,7 +775,7 @@ def rom_step_q4(dims, weights, q4_group, x, B, conv_state, ssm_state, out, ws):
 
 
 def rom_block_step_q4(dims, weights, q4_group, norm_weight, eps, x, B, conv_state, ssm_state, out, ws):
-    index = _current_index(x)
+    index = _expect_step(dims, x, B, conv_state, ssm_state, out)
     _expect_projections(dims, weights, q4_group, index)
     _expect_ws(ws, index)
     code = load_library().rom_block_step_q4(
@@ -789,7 +799,9 @@ def _stack_kinds(n_experts: int, d_inner: int, d_model: int, d_ff: int, q4_group
 def rom_hybrid_stack_step(dims, d_ff, blocks, ffns, q4_group, ffn_pre_norm, eps, x, B, conv_state, ssm_state, out, tmp, ws,
                           ffn_ws):
     """blocks, ffns: make_blocks, make_ffns (arrays put together otherwise are taken as they are)."""
-    index, dtype = _current_index(x), _TORCH_TYPE.get(dims.dtype)
+    index, dtype = _expect_step(dims, x, B, conv_state, ssm_state, out, (len(blocks),)), _TORCH_TYPE.get(dims.dtype)
+    if tmp is not None and (tmp.dtype is not dtype or tmp.numel() != x.numel() or tmp.get_device() != index):
+        raise RomError(f"tmp: expected {x.numel()} values of {dtype} on cuda:{index}, got {tmp.numel()} of {tmp.dtype} on {tmp.device}")
     if q4_group >= 0 and dtype is not None:         # else the library refuses it
         for arr, what, want in zip((blocks, ffns), ("blocks", "ffns"),
                                    _stack_kinds(dims.n_experts, dims.d_inner, dims.d_model, d_ff, q4_group, dtype, index)):
@@ -901,18 +913,10 @@ class RomLayer:
         _keep_if_captured(self._kept, self._ws)
         return self._ws
 
-    def _check_step(self, x, conv_state, ssm_state, out):
-        B, d, index = x.shape[0], self.dims, _current_index(x)
-        _expect(x, "x", self.tdtype, (B, d.d_model), index)
-        _expect(out, "out", self.tdtype, (B, d.d_model), index)
-        _expect(conv_state, "conv_state", torch.float32, (B, d.d_inner, d.d_conv - 1), index)
-        _expect(ssm_state, "ssm_state", torch.float32, (B, d.d_inner, d.d_state), index)
-
     def step_q4(self, x: torch.Tensor, conv_state: torch.Tensor, ssm_state: torch.Tensor, group: int = 64,
                 out: Optional[torch.Tensor] = None):
         """step with w_in and w_out in 4 bits (rom_step_q4): up to ROM_FEW_TOKENS sequences."""
         out = torch.empty_like(x) if out is None else out
-        self._check_step(x, conv_state, ssm_state, out)
         rom_step_q4(self.dims, self.q4_weights(group), group, x, x.shape[0], conv_state, ssm_state, out,
                     self.workspace_q4(max(x.shape[0], 1)))
         return out
@@ -920,7 +924,6 @@ class RomLayer:
     def block_step_q4(self, x: torch.Tensor, conv_state: torch.Tensor, ssm_state: torch.Tensor, group: int = 64,
                       out: Optional[torch.Tensor] = None, eps: float = 1e-5):
         out = torch.empty_like(x) if out is None else out
-        self._check_step(x, conv_state, ssm_state, out)
         rom_block_step_q4(self.dims, self.q4_weights(group, block=True), group, self.weights["norm_w"], eps, x, x.shape[0],
                           conv_state, ssm_state, out, self.workspace_q4(max(x.shape[0], 1)))
         return out
@@ -1379,13 +1382,9 @@ class RomHybridStack:
         4-bit weights of that group."""
         B = x.shape[0]
         out = torch.empty_like(x) if out is None else out
-        layer, index = self.layers[0], _current_index(x)
-        _expect(x, "x", layer.tdtype, (B, self.dims.d_model), index)
-        _expect(out, "out", x.dtype, x.shape, index)
-        for t, what, shape in zip((conv_state, ssm_state), ("conv_state", "ssm_state"), self.state_shapes(B)):
-            _expect(t, what, torch.float32, shape, index)
+        layer = self.layers[0]
         if self._tmp is None or self._tmp.numel() != x.numel() or self._tmp.dtype != x.dtype:
-            self._tmp = torch.empty_like(x)
+            self._tmp = torch.empty(x.shape, dtype=x.dtype, device=self.device)      # also where x turns out to lie elsewhere
         need = rom_hybrid_step_ffn_workspace_bytes(self.dims, self.d_ff, max(B, 1), q4_group)
         if need == 0:
             raise RomError("rom_hybrid_step_ffn_workspace_bytes returned 0: unsupported dims, d_ff, group or batch")

@@ -243,3 +243,48 @@ def test_workspaces_elsewhere_or_with_gaps(host):
             with pytest.raises(binding.RomError):
                 call(ws)
         assert len(host.lib.calls) == n
+
+
+def test_raw_steps_refuse_what_the_holders_refuse(host):
+    """The wrappers of the C ABI see types, shapes and devices; the library sees addresses."""
+    layer, B = layer_of(), 3
+    x, (cs, ss) = tokens(B)[0], states(B)
+    bad = [dict(x=x.float()), dict(x=x[:, :32].contiguous()), dict(out=x[:2].clone()), dict(out=x.float()), dict(conv_state=cs.bfloat16()),
+           dict(conv_state=cs[:2].contiguous()), dict(ssm_state=ss.transpose(1, 2)), dict(ssm_state=ss.double()), dict(out=x.clone().as_subclass(Elsewhere)),
+           dict(ssm_state=ss.clone().as_subclass(Elsewhere)), dict(B=4), dict(weights={k: v if k != "w_in" else v.as_subclass(Elsewhere)
+                                                                                       for k, v in layer.q4_weights(32).items()})]
+    for call in raw_steps(layer, 32, layer.q4_weights(32)):
+        for kw in bad:
+            with pytest.raises(binding.RomError):
+                call(**kw)
+    for group in (0, 32):
+        stack = hybrid_of(2)
+        stack.quantize(32)
+        blocks, ffns = (stack.blocks, stack.ffn_structs) if group == 0 else stack._q4[32][:2]
+        cs, ss = states(B, 2)
+        base = dict(dims=stack.dims, d_ff=F, blocks=blocks, ffns=ffns, q4_group=group, ffn_pre_norm=True, eps=1e-5, x=x, B=B, conv_state=cs, ssm_state=ss,
+                    out=x.clone(), tmp=x.clone(), ws=torch.zeros(1 << 20, dtype=torch.uint8), ffn_ws=torch.zeros(1 << 20, dtype=torch.uint8))
+        for kw in (dict(x=x.float()), dict(out=x[:2].clone()), dict(tmp=x[:2].clone()), dict(tmp=x.float()), dict(conv_state=cs[:1].contiguous()), dict(ssm_state=ss[0]),
+                   dict(B=2), dict(tmp=x.clone().as_subclass(Elsewhere))):
+            with pytest.raises(binding.RomError):
+                binding.rom_hybrid_stack_step(**dict(base, **kw))
+    assert host.lib.calls.count("rom_step_q4") + host.lib.calls.count("rom_hybrid_stack_step") == 0
+
+
+def test_steps_of_a_layer_on_another_device(host):
+    """x and the states agree with each other; the layer's weights lie elsewhere."""
+    layer = layer_of()
+    x, (cs, ss) = tokens(3)[0], states(3)
+    layer.step_q4(x, cs, ss), layer.block_step_q4(x, cs, ss)
+    stack = hybrid_of(2)
+    stack.step(x, *states(3, 2)), stack.step(x, *states(3, 2), q4_group=32)
+    n = len(host.lib.calls)
+    x, cs, ss = (t.as_subclass(Elsewhere) for t in (x, cs, ss))
+    stack._tmp = None
+    for call in (lambda: layer.step_q4(x, cs, ss, out=x.clone()), lambda: layer.block_step_q4(x, cs, ss, out=x.clone()),
+                 lambda: stack.step(x, *(t.as_subclass(Elsewhere) for t in states(3, 2)), out=x.clone()),
+                 lambda: stack.step(x, *(t.as_subclass(Elsewhere) for t in states(3, 2)), 32, out=x.clone())):
+        with pytest.raises(binding.RomError):
+            call()
+    assert len(host.lib.calls) == n
+    stack.step(tokens(3)[0], *states(3, 2))                     # what a refused call left behind serves the next
