@@ -288,3 +288,38 @@ def test_steps_of_a_layer_on_another_device(host):
             call()
     assert len(host.lib.calls) == n
     stack.step(tokens(3)[0], *states(3, 2))                     # what a refused call left behind serves the next
+
+
+# ---------------------------------------------------------------- the C entry of the stack's step
+
+
+@pytest.fixture
+def entry():
+    """rom_hybrid_stack_step of RoM + FFN-MoE pairs on addresses that a call which launches nothing does not touch."""
+    import ctypes
+    import os
+    if not os.path.exists(binding._LIB_PATH):
+        build_library()
+    lib, buf = binding.load_library(), ctypes.create_string_buffer(1 << 16)
+    at = (ctypes.addressof(buf) + 255) // 256 * 256
+    d = binding.RomDims(D, DE, 16, 4, 8, E, 1, E, 1, 0)
+
+    def call(n=1, B=4, x=at, out=at + 8192, tmp=at + 16384, ffn=True, group=0):
+        blocks, ffns = (binding._RomBlock * n)(), (binding._RomFfnWeights * n)()
+        for j in range(n):
+            blocks[j].w, blocks[j].norm_weight = binding._RomWeights(*([at] * 11)), at
+            if ffn:
+                ffns[j] = binding._RomFfnWeights(at, at)
+        return lib.rom_hybrid_stack_step(ctypes.byref(d), F, blocks, ffns, group, 1, n, ctypes.c_float(1e-5), x, B, at, at, out, tmp, at, 1 << 40,
+                                         at + 32768, 1 << 40, None)
+
+    call.at, call.keep = at, buf
+    return call
+
+
+@pytest.mark.parametrize("group", [0, 32])
+@pytest.mark.parametrize("n,ffn", [(1, True), (2, False), (3, True), (1, False), (3, False)])
+def test_a_stack_step_is_refused_before_a_state_moves(entry, n, ffn, group):
+    """The first block of an even number of them writes tmp: an output that the last one cannot write is seen before."""
+    assert entry(n=n, ffn=ffn, group=group, out=entry.at + 8200) == -1
+    assert entry(n=n, ffn=ffn, group=group, x=entry.at + 8) == -1
