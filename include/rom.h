@@ -526,6 +526,7 @@ ROM_API int rom_block_step_q4(const rom_dims *dims, const rom_weights *w, int32_
  * 128: w_in, w_out and both FFN weights of every layer are packed by rom_q4_pack with that group (B at most
  * ROM_FEW_TOKENS then).  Every FFN-MoE block runs on the decision of the RoM block in front of it: as rom_ffn_moe_step
  * with q4_group, in fp32 and for bf16 weights that few slots share, otherwise (and beyond ROM_FEW_TOKENS) as rom_ffn_moe_forward.
+ * A refused call has launched nothing and moved no state; B == 0 is a successful no-op.
  *   ws      rom_workspace_bytes(dims, B, 1), with q4_group rom_step_q4_workspace_bytes(dims, B)
  *   ffn_ws  rom_hybrid_step_ffn_workspace_bytes(dims, d_ff, B, q4_group), distinct from ws (may be NULL if no layer has
  *           an FFN) */

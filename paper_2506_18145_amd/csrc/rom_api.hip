@@ -1441,9 +1441,9 @@ int rom_hybrid_stack_step(const rom_dims *dims, int32_t d_ff, const rom_block *b
       n_ops += 1;
     }
   }
+  if (B == 0) return ROM_OK;            // whatever the buffers: empty ones have no address
   const bool any_ffn = n_ops > n_layers;
   if (n_ops > 1 && (!tmp || tmp == x || tmp == out || !aligned16(tmp))) return ROM_E_INVAL;
-  if (B == 0) return ROM_OK;
   if (!x || !out || x == out || !conv_state || !ssm_state || !ws || (any_ffn && (!ffn_ws || ffn_ws == ws))) return ROM_E_INVAL;
   if (!aligned16(x) || !aligned16(out)) return ROM_E_INVAL;      // a first block that writes tmp would not see out
   if (any_ffn && (reinterpret_cast<uintptr_t>(ffn_ws) % kAlign) != 0) return ROM_E_INVAL;

@@ -323,3 +323,11 @@ def test_a_stack_step_is_refused_before_a_state_moves(entry, n, ffn, group):
     """The first block of an even number of them writes tmp: an output that the last one cannot write is seen before."""
     assert entry(n=n, ffn=ffn, group=group, out=entry.at + 8200) == -1
     assert entry(n=n, ffn=ffn, group=group, x=entry.at + 8) == -1
+
+
+@pytest.mark.parametrize("group", [0, 32])
+def test_a_stack_step_of_no_sequences_does_nothing(entry, host, group):
+    assert entry(n=3, B=0, x=None, out=None, tmp=None, group=group) == 0       # empty tensors have no address
+    assert entry(n=3, B=0, x=entry.at, out=entry.at, tmp=entry.at, group=group) == 0
+    stack = hybrid_of(2)
+    assert stack.step(tokens(0)[0], *states(0, 2), q4_group=group).shape == (0, D)

@@ -81,3 +81,15 @@ def test_a_captured_plain_step_replayed_behind_4_bit_steps(block):
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(cs, want_cs) and torch.equal(ss, want_ss)
         assert all(bool((f == -1).all()) for f in fill)
+
+
+@pytest.mark.parametrize("group", [0, 64])
+def test_a_stack_step_of_no_sequences(group):
+    cfg = step_cfg(batch=0)
+    stack = hybrid(cfg)
+    x, (cs, ss) = randn(1, 0, cfg.d_model), states(cfg, 2, 3)
+    assert stack.step(x, cs, ss, q4_group=group).shape == (0, cfg.d_model)
+    layer, ffn = stack.layers[0], stack.ffns[0]
+    assert layer.step_q4(x, cs[0], ss[0]).shape == x.shape and layer.block_step_q4(x, cs[0], ss[0]).shape == x.shape
+    idx, gate = torch.empty((0, 1), dtype=torch.int32, device=x.device), torch.empty((0, 1), device=x.device)
+    assert ffn.step(x, idx, gate, True, True, group).shape == x.shape
