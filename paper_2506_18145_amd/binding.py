@@ -898,6 +898,8 @@ class RomLayer:
         in 4 bits, packed once, everything else shared with the plain layer."""
         if (group, block) not in self._q4:
             _not_while_capturing("q4_weights")
+            if not block and self._block_weights is not None and self._block_weights["w_in"] is self.weights["w_in"]:
+                raise RomError("w_in has been folded in place with the pre-norm's scale: only block_step_q4 is meaningful")
             w = dict(self.block_weights() if block else self.weights)
             w["w_in"] = RomQ4Weight.pack(w["w_in"], group).packed
             w["w_out"] = RomQ4Weight.pack(w["w_out"], group).packed

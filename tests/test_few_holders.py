@@ -331,3 +331,18 @@ def test_a_stack_step_of_no_sequences_does_nothing(entry, host, group):
     assert entry(n=3, B=0, x=entry.at, out=entry.at, tmp=entry.at, group=group) == 0
     stack = hybrid_of(2)
     assert stack.step(tokens(0)[0], *states(0, 2), q4_group=group).shape == (0, D)
+
+
+def test_plain_4_bit_weights_are_not_packed_from_folded_ones(host):
+    """A stack folds its layers' norms into w_in in place: the layer's own step would get the scale that belongs to the block."""
+    x, (cs, ss) = tokens(3)[0], states(3)
+    layer, early = layer_of(), layer_of()
+    early.step_q4(x, cs, ss)                                    # packed from the plain weights
+    for ly in (layer, early):
+        binding.RomHybridStack([ly], [ffn_of(ly)])
+    with pytest.raises(binding.RomError, match="folded"):
+        layer.step_q4(x, cs, ss)
+    layer.block_step_q4(x, cs, ss), early.step_q4(x, cs, ss)
+    apart = layer_of()
+    binding.RomHybridStack([apart], [None], fold_in_place=False)
+    apart.step_q4(x, cs, ss)

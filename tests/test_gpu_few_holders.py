@@ -90,6 +90,7 @@ def test_a_stack_step_of_no_sequences(group):
     x, (cs, ss) = randn(1, 0, cfg.d_model), states(cfg, 2, 3)
     assert stack.step(x, cs, ss, q4_group=group).shape == (0, cfg.d_model)
     layer, ffn = stack.layers[0], stack.ffns[0]
-    assert layer.step_q4(x, cs[0], ss[0]).shape == x.shape and layer.block_step_q4(x, cs[0], ss[0]).shape == x.shape
+    plain = ffn_holder(cfg.d_model, 32, 4, 1, "bf16")[1]
+    assert plain.step_q4(x, cs[0], ss[0]).shape == x.shape and layer.block_step_q4(x, cs[0], ss[0]).shape == x.shape
     idx, gate = torch.empty((0, 1), dtype=torch.int32, device=x.device), torch.empty((0, 1), device=x.device)
     assert ffn.step(x, idx, gate, True, True, group).shape == x.shape
