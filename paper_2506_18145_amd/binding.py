@@ -816,6 +816,11 @@ def rom_hybrid_stack_step(dims, d_ff, blocks, ffns, q4_group, ffn_pre_norm, eps,
     _check(code, "rom_hybrid_stack_step")
 
 
+def _room_for(n_tokens: int) -> int:
+    """Tokens that a holder's workspace for a call of so many is made for: the next power of two, at most ROM_FEW_TOKENS."""
+    return min(1 << max(n_tokens - 1, 0).bit_length(), ROM_FEW_TOKENS)
+
+
 class RomQ4Weight:
     """A stack of matrices [n_mats, rows, cols] held in 4 bits with a scale per row and `group` columns.  The calls of one
     holder share its workspace: they go to one stream, or wait for each other."""
@@ -830,7 +835,7 @@ class RomQ4Weight:
         _expect(packed, "packed", torch.uint8, (need,), self.index)
         self.packed, self.n_mats, self.rows, self.cols, self.group = packed, n_mats, rows, cols, group
         self.device = packed.device
-        self._ws: Dict[int, Optional[torch.Tensor]] = {}      # by top_k, for ROM_FEW_TOKENS tokens: never replaced
+        self._ws: Dict[tuple, Optional[torch.Tensor]] = {}    # by top_k and _room_for: never replaced, captured calls go on with theirs
 
     @classmethod
     def pack(cls, w: torch.Tensor, group: int = 64) -> "RomQ4Weight":
@@ -854,11 +859,12 @@ class RomQ4Weight:
             out = torch.empty((x.shape[0], self.rows), dtype=x.dtype, device=x.device)
         if x.get_device() != self.index:
             raise RomError(f"x on {x.device}, the weights on {self.device}")
-        if k not in self._ws:
-            need = rom_q4_project_workspace_bytes(self.rows, k, ROM_FEW_TOKENS)
-            self._ws[k] = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+        room = _room_for(x.shape[0])
+        if (k, room) not in self._ws:
+            need = rom_q4_project_workspace_bytes(self.rows, k, room)
+            self._ws[k, room] = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
         _q4_project(self.packed, self.n_mats, self.rows, self.cols, self.group, x, k, expert_idx, gate, row_scale, residual, out,
-                    self._ws[k])
+                    self._ws[k, room])
         return out
 
 
@@ -1199,7 +1205,7 @@ class RomFfnMoe:
         self._packed: Dict[bool, torch.Tensor] = {}
         self._q4: Dict[tuple, tuple] = {}
         self._ws: Optional[torch.Tensor] = None
-        self._step_ws: Optional[torch.Tensor] = None
+        self._step_ws: Dict[int, torch.Tensor] = {}           # by _room_for: never replaced, captured calls go on with theirs
         self._bwd_ws: Optional[torch.Tensor] = None
 
     def q4_weights(self, group: int, pre_norm: bool):
@@ -1219,14 +1225,15 @@ class RomFfnMoe:
         if not q4_group and bool(pre_norm) not in self._packed:
             _not_while_capturing("RomFfnMoe.step")
         out = torch.empty_like(x) if out is None else out
-        if self._step_ws is None:             # for ROM_FEW_TOKENS tokens: never replaced
-            need = rom_ffn_step_workspace_bytes(d, self.d_ff, ROM_FEW_TOKENS)
+        room = _room_for(n)
+        if room not in self._step_ws:
+            need = rom_ffn_step_workspace_bytes(d, self.d_ff, room)
             if need == 0:
                 raise RomError("rom_ffn_step_workspace_bytes returned 0: unsupported dims or d_ff")
-            self._step_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+            self._step_ws[room] = torch.empty(need, dtype=torch.uint8, device=self.device)
         gu, down = self.q4_weights(q4_group, pre_norm) if q4_group else (self.packed(bool(pre_norm)), self.w_down)
         rom_ffn_moe_step(d, self.d_ff, gu, down, q4_group, pre_norm, self.eps, add_skip, x, n, expert_idx, gate, out,
-                         self._step_ws)
+                         self._step_ws[room])
         return out
 
     def packed(self, pre_norm: bool, drop_plain: bool = False) -> torch.Tensor:

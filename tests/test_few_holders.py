@@ -346,3 +346,37 @@ def test_plain_4_bit_weights_are_not_packed_from_folded_ones(host):
     apart = layer_of()
     binding.RomHybridStack([apart], [None], fold_in_place=False)
     apart.step_q4(x, cs, ss)
+
+
+# ---------------------------------------------------------------- workspaces
+
+
+def test_workspaces_are_sized_by_the_call(host, monkeypatch):
+    """One token through wide matrices asks for one token's partial sums; what a size has got is never replaced."""
+    asked = []
+    empty = torch.empty
+
+    def counted(*size, **kw):
+        out = empty(*size, **kw)
+        if out.dtype is torch.uint8:
+            asked.append(out.numel())
+        return out
+
+    q = binding.RomQ4Weight.__new__(binding.RomQ4Weight)
+    q.packed, q.n_mats, q.rows, q.cols, q.group = packed_of(1 << 14, D), E, 1 << 14, D, 32
+    q.device, q.index, q._ws = torch.device("cpu"), -1, {}
+    ffn = ffn_of(layer_of(top_k=2))
+    monkeypatch.setattr(torch, "empty", counted)
+    need = {"project": lambda n: binding.rom_q4_project_workspace_bytes(q.rows, 2, n),
+            "step": lambda n: binding.rom_ffn_step_workspace_bytes(ffn.dims, F, n)}
+    for what, call in (("project", lambda n: q.project(tokens(n)[0], *tokens(n, 2)[1:])), ("step", lambda n: ffn.step(*tokens(n, 2), True))):
+        for n in (1, 2, 3, 5, 100, 256):
+            asked.clear()
+            call(n)
+            call(n)
+            assert len(asked) <= 1 and need[what](n) <= sum(asked) < 2 * need[what](n)      # up to the next power of two
+        asked.clear()
+        for n in (1, 2, 4, 7, 128, 129, 256, 6):
+            call(n)
+        assert not asked
+    assert need["project"](256) == 256 * need["project"](1)
