@@ -501,7 +501,7 @@ ROM_API int rom_q4_project(int dtype, const void *w_q4, int32_t n_mats, int32_t 
  *   expert_idx   i32 [N, K], gate f32 [N, K]: as rom_route, a layer call or a step left them; expert_idx as above
  *   pre_norm, eps, add_skip, x, out   as rom_ffn_moe_forward
  *   ws           rom_ffn_step_workspace_bytes(dims, d_ff, N), 256-byte aligned
- * SiLU(gate) * up is rounded to T between the launches; every sum is fp32.  N at most ROM_FEW_TOKENS, d_ff at most
+ * SiLU(gate) * up is rounded to T between the launches; every sum is fp32.  SiLU(a) is a * sigmoid(a): a gate of -infinity gives NaN.  N at most ROM_FEW_TOKENS, d_ff at most
  * 2^19, d_model 2^20.  Repeated calls give identical bits; a token's result does not depend on the other tokens of a call of
  * the same N.  (bf16 weights read by more than about eight slots an expert are faster through rom_ffn_moe_forward.) */
 ROM_API size_t rom_ffn_step_workspace_bytes(const rom_dims *dims, int32_t d_ff, int64_t N);
