@@ -601,10 +601,14 @@ def _expect(t: Optional[torch.Tensor], what: str, dtype, shape, index: int) -> N
                        f"{tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
 
 
+# the current device without the look whether CUDA has started: a tensor is there
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _current_index(t: torch.Tensor) -> int:
     """Index of t's device, which has to be the current one: the calls go to its current stream."""
     index = t.get_device()
-    if index < 0 or index != torch.cuda.current_device():
+    if index < 0 or index != _current_device():
         raise RomError(f"a tensor on {t.device}, which is not the current device")
     return index
 
@@ -816,9 +820,12 @@ def rom_hybrid_stack_step(dims, d_ff, blocks, ffns, q4_group, ffn_pre_norm, eps,
     _check(code, "rom_hybrid_stack_step")
 
 
+# tokens that a holder's workspace for a call of n of them is made for: the next power of two
+_ROOM = tuple(1 << max(n - 1, 0).bit_length() for n in range(ROM_FEW_TOKENS + 1))
+
+
 def _room_for(n_tokens: int) -> int:
-    """Tokens that a holder's workspace for a call of so many is made for: the next power of two, at most ROM_FEW_TOKENS."""
-    return min(1 << max(n_tokens - 1, 0).bit_length(), ROM_FEW_TOKENS)
+    return _ROOM[n_tokens] if n_tokens <= ROM_FEW_TOKENS else ROM_FEW_TOKENS      # the library refuses more
 
 
 class RomQ4Weight:
