@@ -308,7 +308,7 @@ __device__ __forceinline__ void few_store4(const FewArgs &a, int n, int row, f32
 // A column is one of the token's up to eight slots, so that an expert that it names twice is nothing special.  Plain rows: the
 // two parts are the halves of a 128-byte line (64 columns).  4 bits: neighbouring blocks.
 // SWIGLU (one slot): eight gate and eight up rows.  Else the workgroup meets the token's experts in turn and adds its slots: no
-// launch for that.  d_model 2048, d_ff 4096: bf16 9.4 + 6.3 us (10.5 + 8.1 by many_slots_kernel), 4 bits down 4.8 (5.8).
+// launch for that.  d_model 2048, d_ff 4096: bf16 9.5 + 5.8 us (10.9 + 7.3 by many_slots_kernel), 4 bits down 4.5 (5.7).
 template <typename T, int G, bool SWIGLU>
 __global__ __launch_bounds__(512) void one_token_kernel(const FewArgs a) {
   constexpr int WAVES = 8, SLOTS = 8, RT = SWIGLU ? 2 : 1;
@@ -934,14 +934,16 @@ void launch_shared(const FewArgs &a, hipStream_t s) {
 }
 
 // Which kernel takes a call.  Times in us, kernels alone, d_model 2048, d_ff 4096, 8 experts, top-1 unless another size stands
-// there; both sides with find_piece, many_slots_kernel up to 64 slots thus 0.5 to 1 longer than with find_piece_64.
-//  one token             one_token_kernel, but for gate | up in 4 bits (6.3 against 7.2) and 4-bit projections of 4096 rows and
-//                        more (8192 x 2048: 5.4 against 7.2), which have row tiles enough for the other kernel
+// there.
+//  one token             one_token_kernel (2048 x 4096 in 4 bits 4.4 against 5.4, top-2 6.0 against 6.0 and a launch for the sums; fp32 512 x 1024
+//                        4.5 against 7.4; worse only for a small gate | up, fp32 2048 x 512 6.4 against 5.1), but for gate | up in 4 bits (no such form; many_slots_kernel 5.8) and 4-bit projections of 4096
+//                        rows and more, which have row tiles enough for the other kernel (4096 x 2048: 4.6 against 5.8; 8192: 4.9 against 9.1)
 //  many slots an expert  shared_slots_kernel where the weights are no longer most of what comes into a CU.  Gate | up, 4 bits:
-//                        32 slots 29.5 against 39.8, 16 24.4 against 27.4, 8 21.5 against 18.8.  bf16: 32 slots 70 + 41 against
-//                        92 + 57, 4 67 + 38 against 55 + 29.  Not the 4-bit projection (32 slots 23.7 against 28.9).
+//                        32 slots 29.5 against 39.8, 16 24.4 against 27.4, 8 23.2 against 18.3.  bf16: 32 slots 70 + 41 against
+//                        92 + 57, 8 68 + 38 against 60 + 37, 4 68 + 39 against 55 + 31.  Not the 4-bit projection (32 slots 23.7 against 28.9).
 //  else                  many_slots_kernel: few row tiles in short calls (enough workgroups), more in long ones (less of x read);
 //                        eight wavefronts where the contraction is deep and workgroups are few.
+//    (two sides of one kernel up to 64 slots: both with find_piece, 0.5 to 1 longer than with find_piece_64)
 //    4 bits  gate | up: four row tiles from 512 workgroups on (4 tokens 10.2; two: 10.1; 8 tokens 12.7, 14.2), two below (512 x 1024, 64
 //            tokens 5.6; four: 6.4).  Projection: two tiles with eight wavefronts up to 512 workgroups (4 tokens 6.5 against
 //            8.1 with four), with four beyond (64 tokens 12.5 against 13.6); four tiles from 8 slots an expert on (32: 23.7
@@ -949,7 +951,9 @@ void launch_shared(const FewArgs &a, hipStream_t s) {
 //    bf16    two tiles; the projection up to 4 slots an expert one with eight wavefronts (4: 29 against 37; 8 slots of 1024 x 2048:
 //            12.6 against 11.3).
 //    fp32    two tiles from 512 workgroups on (100 tokens through 4096 x 1024 in 4 bits 21.6 against 27.3), one below (8 tokens of
-//            512 x 1024 9.8 against 10.8), from 2048 columns on with eight wavefronts.
+//            512 x 1024 9.8 against 10.8), from 2048 columns on with eight wavefronts.  Eight against four, four experts, 3 tokens, 1024 rows:
+//            4-bit projection of 4096 columns 10.1 / 12.3, 2048 6.7 / 7.7, 1536 6.0 / 6.6, 512 4.5 / 4.5; plain gate | up 18.0 / 22.0,
+//            12.5 / 14.1, 10.4 / 11.3, 5.1 / 5.1.  Shorter rows do not bear them everywhere: 2072 x 1048 top-2 5 tokens 9.3 / 9.6, 60 17.3 / 15.6.
 constexpr int kOneTokenRows = 4096;
 constexpr int kManyAvg = 8;
 
