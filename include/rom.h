@@ -493,17 +493,18 @@ ROM_API int rom_q4_project(int dtype, const void *w_q4, int32_t n_mats, int32_t 
                            void *hip_stream);
 
 /* The FFN-MoE layer of rom_ffn_moe_forward for a few tokens: pre-norm, gate | up, SwiGLU, down, gate-weighted sum
- * and skip in two launches (three with top_k > 1 and several tokens), straight from the routing decision,
- * without its grouping.
+ * and skip in two launches, straight from the routing decision, without its grouping.  With top_k > 1 a third one
+ * adds a token's slots, for several tokens and for one whose weights are in 4 bits with d_model at least 4096.
  *   w            q4_group 0: as rom_ffn_moe_forward takes them (w_gate_up in the packed row order).  q4_group
  *                32, 64 or 128: both packed by rom_q4_pack with that group (w_gate_up after
  *                rom_ffn_pack_gate_up: [E, 2*d_ff, d_model] and [E, d_model, d_ff])
  *   expert_idx   i32 [N, K], gate f32 [N, K]: as rom_route, a layer call or a step left them; expert_idx as above
  *   pre_norm, eps, add_skip, x, out   as rom_ffn_moe_forward
  *   ws           rom_ffn_step_workspace_bytes(dims, d_ff, N), 256-byte aligned
- * SiLU(gate) * up is rounded to T between the launches; every sum is fp32.  SiLU(a) is a * sigmoid(a): a gate of -infinity gives NaN.  N at most ROM_FEW_TOKENS, d_ff at most
- * 2^19, d_model 2^20.  Repeated calls give identical bits; a token's result does not depend on the other tokens of a call of
- * the same N.  (bf16 weights read by more than about eight slots an expert are faster through rom_ffn_moe_forward.) */
+ * SiLU(gate) * up is rounded to T between the launches; every sum is fp32.  SiLU(a) is a * sigmoid(a): a gate of -infinity gives NaN.
+ * N at most ROM_FEW_TOKENS, d_ff at most 2^19, d_model 2^20.  Repeated calls give identical bits; a token's result does not
+ * depend on the other tokens of a call of the same N.  (Plain bf16 weights of eight experts and more are faster through
+ * rom_ffn_moe_forward from about 8 slots an expert on at d_model 2048, 16 at 1024; fp32 and 4-bit weights never are.) */
 ROM_API size_t rom_ffn_step_workspace_bytes(const rom_dims *dims, int32_t d_ff, int64_t N);
 ROM_API int rom_ffn_moe_step(const rom_dims *dims, int32_t d_ff, const rom_ffn_weights *w, int32_t q4_group, int pre_norm,
                              float eps, int add_skip, const void *x, int64_t N, const int32_t *expert_idx,

@@ -1343,7 +1343,10 @@ FfnStepPlan make_ffn_step_plan(const rom_dims *d, int32_t d_ff, int64_t N) {
 // Whether the FFN-MoE block of a hybrid step runs as rom_ffn_moe_step.  bf16 weights read by many slots an expert are better off with
 // the grouped GEMM, as the RoM block has left the grouping: d_model 2048, d_ff 4096, us: 8 experts, 4 tokens 39 against
 // 42, 16 74 / 86, 64 93 / 90, 256 114 / 93; 16 experts top-2, 32 tokens 158 / 164, 64 176 / 164; d_model 1024, 64 tokens 29 / 35, 256
-// 43 / 36.  fp32 (d_model 512) 8 tokens 24 / 42, 256 73 / 92.
+// 43 / 36.  With one or two experts the grouped GEMM has few workgroups, and the line lies further out than it is drawn here: d_model 2048, two
+// experts, 32 tokens 40 / 61, 128 65 / 65.  fp32: the grouped GEMM is never ahead, also with all slots on one expert: d_model 512 256 tokens
+// 33 / 53, eight experts top-2 8 tokens 24 / 42, 256 73 / 92; d_model 2048 one expert 16 tokens 46 / 149, 256 353 / 492, eight 416 / 593, top-2
+// 736 / 985; d_model 1024 one expert 256 tokens 97 / 154.
 bool hybrid_ffn_by_step(const rom_dims *d, int64_t B, int32_t q4_group) {
   if (q4_group) return true;                             // B was checked
   if (B > ROM_FEW_TOKENS) return false;
