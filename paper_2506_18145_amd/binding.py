@@ -759,7 +759,8 @@ def _expect_projections(dims, weights, q4_group: int, index: int) -> None:
 
 
 def _expect_step(dims, x, B: int, conv_state, ssm_state, out, lead: tuple = ()) -> int:
-    """One token of each of B sequences and the states of one layer (lead (): else of so many); x's device index."""
+    """What a holder's step takes: one token of each of B sequences and the states of one layer (lead (): else of so many);
+    x's device index."""
     index, dtype = _current_index(x), _TORCH_TYPE.get(dims.dtype)
     _expect(x, "x", dtype, (B, dims.d_model), index)
     _expect(out, "out", dtype, (B, dims.d_model), index)
@@ -768,8 +769,27 @@ def _expect_step(dims, x, B: int, conv_state, ssm_state, out, lead: tuple = ()) 
     return index
 
 
+def _expect_room(t: Optional[torch.Tensor], what: str, dtype, count: int, index: int) -> None:
+    if t is not None and (t.dtype is not dtype or t.numel() < count or t.get_device() != index or not t.is_contiguous()):
+        raise RomError(f"{what}: expected {count} contiguous values of {dtype} or more on cuda:{index}, got {t.dtype} {tuple(t.shape)} "
+                       f"on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
+
+
+def _expect_step_room(dims, x, B: int, conv_state, ssm_state, out, n_layers: int = 1) -> int:
+    """The same for the C ABI's wrappers, whose B may be less than their buffers have room for."""
+    index, dtype = _current_index(x), _TORCH_TYPE.get(dims.dtype)
+    _expect_room(x, "x", dtype, B * dims.d_model, index)
+    _expect_room(out, "out", dtype, B * dims.d_model, index)
+    _expect_room(conv_state, "conv_state", torch.float32, n_layers * B * dims.d_inner * (dims.d_conv - 1), index)
+    _expect_room(ssm_state, "ssm_state", torch.float32, n_layers * B * dims.d_inner * dims.d_state, index)
+    return index
+
+
 def rom_step_q4(dims, weights, q4_group, x, B, conv_state, ssm_state, out, ws):
-    index = _expect_step(dims, x, B, conv_state, ssm_state, out)
+    _step_q4(dims, weights, q4_group, x, B, conv_state, ssm_state, out, ws, _expect_step_room(dims, x, B, conv_state, ssm_state, out))
+
+
+def _step_q4(dims, weights, q4_group, x, B, conv_state, ssm_state, out, ws, index):
     _expect_projections(dims, weights, q4_group, index)
     _expect_ws(ws, index)
     code = load_library().rom_step_q4(
@@ -779,7 +799,11 @@ def rom_step_q4(dims, weights, q4_group, x, B, conv_state, ssm_state, out, ws):
 
 
 def rom_block_step_q4(dims, weights, q4_group, norm_weight, eps, x, B, conv_state, ssm_state, out, ws):
-    index = _expect_step(dims, x, B, conv_state, ssm_state, out)
+    _block_step_q4(dims, weights, q4_group, norm_weight, eps, x, B, conv_state, ssm_state, out, ws,
+                   _expect_step_room(dims, x, B, conv_state, ssm_state, out))
+
+
+def _block_step_q4(dims, weights, q4_group, norm_weight, eps, x, B, conv_state, ssm_state, out, ws, index):
     _expect_projections(dims, weights, q4_group, index)
     _expect_ws(ws, index)
     code = load_library().rom_block_step_q4(
@@ -803,9 +827,13 @@ def _stack_kinds(n_experts: int, d_inner: int, d_model: int, d_ff: int, q4_group
 def rom_hybrid_stack_step(dims, d_ff, blocks, ffns, q4_group, ffn_pre_norm, eps, x, B, conv_state, ssm_state, out, tmp, ws,
                           ffn_ws):
     """blocks, ffns: make_blocks, make_ffns (arrays put together otherwise are taken as they are)."""
-    index, dtype = _expect_step(dims, x, B, conv_state, ssm_state, out, (len(blocks),)), _TORCH_TYPE.get(dims.dtype)
-    if tmp is not None and (tmp.dtype is not dtype or tmp.numel() != x.numel() or tmp.get_device() != index):
-        raise RomError(f"tmp: expected {x.numel()} values of {dtype} on cuda:{index}, got {tmp.numel()} of {tmp.dtype} on {tmp.device}")
+    _hybrid_stack_step(dims, d_ff, blocks, ffns, q4_group, ffn_pre_norm, eps, x, B, conv_state, ssm_state, out, tmp, ws, ffn_ws,
+                       _expect_step_room(dims, x, B, conv_state, ssm_state, out, len(blocks)))
+
+
+def _hybrid_stack_step(dims, d_ff, blocks, ffns, q4_group, ffn_pre_norm, eps, x, B, conv_state, ssm_state, out, tmp, ws, ffn_ws, index):
+    dtype = _TORCH_TYPE.get(dims.dtype)
+    _expect_room(tmp, "tmp", dtype, B * dims.d_model, index)
     if q4_group >= 0 and dtype is not None:         # else the library refuses it
         for arr, what, want in zip((blocks, ffns), ("blocks", "ffns"),
                                    _stack_kinds(dims.n_experts, dims.d_inner, dims.d_model, d_ff, q4_group, dtype, index)):
@@ -932,15 +960,18 @@ class RomLayer:
                 out: Optional[torch.Tensor] = None):
         """step with w_in and w_out in 4 bits (rom_step_q4): up to ROM_FEW_TOKENS sequences."""
         out = torch.empty_like(x) if out is None else out
-        rom_step_q4(self.dims, self.q4_weights(group), group, x, x.shape[0], conv_state, ssm_state, out,
-                    self.workspace_q4(max(x.shape[0], 1)))
+        B = x.shape[0]
+        index = _expect_step(self.dims, x, B, conv_state, ssm_state, out)
+        _step_q4(self.dims, self.q4_weights(group), group, x, B, conv_state, ssm_state, out, self.workspace_q4(max(B, 1)), index)
         return out
 
     def block_step_q4(self, x: torch.Tensor, conv_state: torch.Tensor, ssm_state: torch.Tensor, group: int = 64,
                       out: Optional[torch.Tensor] = None, eps: float = 1e-5):
         out = torch.empty_like(x) if out is None else out
-        rom_block_step_q4(self.dims, self.q4_weights(group, block=True), group, self.weights["norm_w"], eps, x, x.shape[0],
-                          conv_state, ssm_state, out, self.workspace_q4(max(x.shape[0], 1)))
+        B = x.shape[0]
+        index = _expect_step(self.dims, x, B, conv_state, ssm_state, out)
+        _block_step_q4(self.dims, self.q4_weights(group, block=True), group, self.weights["norm_w"], eps, x, B, conv_state,
+                       ssm_state, out, self.workspace_q4(max(B, 1)), index)
         return out
 
     def block_weights(self, in_place: bool = False) -> Dict[str, Optional[torch.Tensor]]:
@@ -1399,8 +1430,9 @@ class RomHybridStack:
         B = x.shape[0]
         out = torch.empty_like(x) if out is None else out
         layer = self.layers[0]
+        index = _expect_step(self.dims, x, B, conv_state, ssm_state, out, (len(self.layers),))
         if self._tmp is None or self._tmp.numel() != x.numel() or self._tmp.dtype != x.dtype:
-            self._tmp = torch.empty(x.shape, dtype=x.dtype, device=self.device)      # also where x turns out to lie elsewhere
+            self._tmp = torch.empty(x.shape, dtype=x.dtype, device=self.device)
         need = rom_hybrid_step_ffn_workspace_bytes(self.dims, self.d_ff, max(B, 1), q4_group)
         if need == 0:
             raise RomError("rom_hybrid_step_ffn_workspace_bytes returned 0: unsupported dims, d_ff, group or batch")
@@ -1409,8 +1441,8 @@ class RomHybridStack:
         blocks, ffns = self.quantize(q4_group)._q4[q4_group][:2] if q4_group else (self.blocks, self.ffn_structs)
         ws = layer.workspace_q4(max(B, 1)) if q4_group else layer.workspace(max(B, 1), 1)
         _keep_if_captured(self._kept, self._tmp, self._ffn_ws, ws)
-        rom_hybrid_stack_step(self.dims, self.d_ff, blocks, ffns, q4_group, self.ffn_pre_norm, self.eps, x, B, conv_state,
-                              ssm_state, out, self._tmp, ws, self._ffn_ws)
+        _hybrid_stack_step(self.dims, self.d_ff, blocks, ffns, q4_group, self.ffn_pre_norm, self.eps, x, B, conv_state, ssm_state, out,
+                           self._tmp, ws, self._ffn_ws, index)
         return out
 
 

@@ -265,7 +265,7 @@ def test_raw_steps_refuse_what_the_holders_refuse(host):
         base = dict(dims=stack.dims, d_ff=F, blocks=blocks, ffns=ffns, q4_group=group, ffn_pre_norm=True, eps=1e-5, x=x, B=B, conv_state=cs, ssm_state=ss,
                     out=x.clone(), tmp=x.clone(), ws=torch.zeros(1 << 20, dtype=torch.uint8), ffn_ws=torch.zeros(1 << 20, dtype=torch.uint8))
         for kw in (dict(x=x.float()), dict(out=x[:2].clone()), dict(tmp=x[:2].clone()), dict(tmp=x.float()), dict(conv_state=cs[:1].contiguous()), dict(ssm_state=ss[0]),
-                   dict(B=2), dict(tmp=x.clone().as_subclass(Elsewhere))):
+                   dict(B=4), dict(tmp=x.clone().as_subclass(Elsewhere))):
             with pytest.raises(binding.RomError):
                 binding.rom_hybrid_stack_step(**dict(base, **kw))
     assert host.lib.calls.count("rom_step_q4") + host.lib.calls.count("rom_hybrid_stack_step") == 0
@@ -380,3 +380,22 @@ def test_workspaces_are_sized_by_the_call(host, monkeypatch):
             call(n)
         assert not asked
     assert need["project"](256) == 256 * need["project"](1)
+
+
+def test_raw_steps_take_buffers_with_room_for_more(host):
+    """B is theirs to say: the tokens, outputs and states of a larger batch, other shapes of as many values."""
+    layer, big = layer_of(), 8
+    cs, ss = states(big)
+    x = torch.zeros(big, 1, D, dtype=torch.bfloat16)
+    for call in raw_steps(layer, 32, layer.q4_weights(32)):
+        for B in (0, 1, 3):
+            call(x=x, out=x.clone(), conv_state=cs, ssm_state=ss, B=B)
+    stack = hybrid_of(2)
+    cs, ss = states(big, 2)
+    binding.rom_hybrid_stack_step(stack.dims, F, stack.blocks, stack.ffn_structs, 0, True, 1e-5, x, 3, cs, ss, x.clone(), x.clone(),
+                                  torch.zeros(1 << 20, dtype=torch.uint8), torch.zeros(1 << 20, dtype=torch.uint8))
+    assert host.lib.calls.count("rom_step_q4") == host.lib.calls.count("rom_block_step_q4") == 3
+    for bad in (lambda: layer.step_q4(x, *states(big)), lambda: layer.block_step_q4(x[:3, 0].contiguous(), *states(big)),
+                lambda: stack.step(x[:3, 0].contiguous(), cs, ss)):
+        with pytest.raises(binding.RomError):                   # a holder's batch is x's
+            bad()
